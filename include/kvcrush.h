@@ -14,6 +14,11 @@
  *   kvcrush_compact  the reduced cache: retained K/V rows gathered into a
  *                    dense layout (Sec. 3.2, last step)
  *
+ * The cache, compressed or not, is then used through kvcrush_cache_write and
+ * kvcrush_cache_read (rows in 8 or 4 bits), kvcrush_attend (attention of new
+ * tokens) and kvcrush_block_bounds / kvcrush_block_select (which blocks a query
+ * attends to).
+ *
  * Conventions common to every entry point
  *   - All data pointers are DEVICE pointers unless a comment says "host".
  *     The argument structs themselves are host memory, read during the call.
@@ -354,9 +359,140 @@ kvcrush_status kvcrush_compact_cache(int32_t B, int32_t Hkv, int32_t Hs, int32_t
                                      const int32_t* idx, void* k_out, void* v_out,
                                      float* scores_out, void* hip_stream);
 
+/* ------------------------------------------------------- using the cache --
+ * One description of a layer's KV cache serves the calls below: dense or paged, in
+ * one of the element types above or in 8 or 4 bits.
+ */
+typedef enum {
+  /* kvcrush_dtype's values, then */
+  KVCRUSH_E4M3 = 3, /* 8-bit floats (4 exponent, 3 mantissa bits, no infinities), one scale a row */
+  KVCRUSH_I8 = 4,   /* integers -127 .. 127, one scale a row                                      */
+  KVCRUSH_I4 = 5    /* integers 0 .. 15, scale and lowest value a row; the even position of a     */
+                    /* row in the low half of its byte                                            */
+} kvcrush_format;
+
+/* A row is one token of one KV head, D values x.  Quantised rows hold, all of it in fp32
+ * with one rounding per operation,
+ *   E4M3, I8   a = max |x|, inv = Q / a (Q = 448, 127), code = x * inv rounded to the
+ *              nearest code (ties to even), parameter s = a / Q; the row's values are code * s.
+ *              a < 2^-100: s = 0 and codes 0.
+ *   I4         lo = min x, d = max x - lo, inv = 15 / d, code = (x - lo) * inv rounded,
+ *              parameters s = d / 15 and lo; the values are lo + s * code (one rounding).
+ *              d < 2^-100: s = 0 and codes 0.
+ * A row with a value (or a difference d) that is not finite gets NaN as its parameters: it
+ * reads back as NaN throughout.
+ */
+typedef struct {
+  int32_t B;           /* sequences                                                              */
+  int32_t Hkv;         /* KV heads                                                               */
+  int32_t S;           /* valid tokens of every sequence, 0 <= S <= capacity; with lengths: their */
+                       /* upper bound                                                            */
+  int32_t D;           /* values per row: 64 or 128                                              */
+  int32_t capacity;    /* tokens a sequence has room for                                         */
+  int32_t format;      /* kvcrush_dtype or kvcrush_format                                        */
+  int32_t block_size;  /* paged caches only: tokens per block; capacity % block_size == 0        */
+  int32_t n_blocks;    /* paged caches only: blocks of the pool, n_blocks * block_size < 2^31    */
+  void* k;             /* dense: [B, Hkv, capacity, D]; paged: [n_blocks, block_size, Hkv, D]    */
+  void* v;             /* (rows of D, or with I4 D / 2, bytes when quantised)                    */
+  float* k_param;      /* quantised only, in k's order: [.., capacity] or [.., block_size, Hkv], */
+  float* v_param;      /* one float a row, with I4 two (scale, lowest value)                     */
+  const int32_t* lengths;     /* NULL, or [B]: each sequence's valid tokens, read by the kernels  */
+                              /* when they run and clamped to [0, S]                             */
+  const int32_t* block_table; /* NULL: dense.  [B, capacity / block_size]: pool block of each    */
+                              /* logical block; an entry outside the pool is pulled into it,     */
+                              /* never followed                                                  */
+} kvcrush_cache;
+
+/* Which of a call's T tokens are real: n_new NULL: all of them, for every sequence.  Otherwise
+ * [B], read by the kernels when they run: the first n_new[b] are, the others are padding.  Values
+ * are clamped to [0, min(T, length)].  The real new tokens are the LAST n of the sequence: token t
+ * stands at position length - n + t.  Lengths count them. */
+
+/* The new tokens' rows enter the cache (quantised as they are written): token t < n of sequence b
+ * goes to position length - n + t.  Rows of no new token are left as they are.
+ *   dtype   of k_new and v_new (kvcrush_dtype); a cache that is not quantised takes its own type only
+ *   k_new, v_new  [B, Hkv, T, D], the D values contiguous; k_stride, v_stride (host): NULL (packed),
+ *           or elements between consecutive sequences, heads and tokens, multiples of 16 bytes
+ * Size limits here and in kvcrush_cache_read: B <= 32767, Hkv <= 65535. */
+kvcrush_status kvcrush_cache_write(const kvcrush_cache* cache, int32_t T, int32_t dtype, const void* k_new,
+                                   const void* v_new, const int64_t* k_stride, const int64_t* v_stride,
+                                   const int32_t* n_new, void* hip_stream);
+
+/* Rows as values again, rounded once to `dtype`: k_out, v_out [B, Hkv, n, D].
+ *   idx     [B, n]: the positions to read (as kvcrush_select writes them); one outside the
+ *           sequence is pulled into it.  NULL: positions 0 .. n - 1, n <= capacity.
+ * Rows that a sequence does not have (position >= length without idx; any row of an empty
+ * sequence) are left as they are in the outputs. */
+kvcrush_status kvcrush_cache_read(const kvcrush_cache* cache, int32_t n, const int32_t* idx, int32_t dtype,
+                                  void* k_out, void* v_out, void* hip_stream);
+
+/* Attention of the T newest tokens, whose rows are in the cache already, over the cache: a decoding
+ * step (T = 1), a drafted chain, or a drafted tree.  With n the real ones of T, query t < n sees
+ *   every position before the new tokens, and
+ *   of the new tokens the j-th iff bit j % 64 of word j / 64 of its mask row is set; without a
+ *   mask, those up to itself.
+ *   out[b, h, t] = sum_j softmax_j(scale q . K[j]) V[j]     lse[b, h, t] = ln sum_j exp(scale q . K[j])
+ * over what it sees.  A query that sees nothing and one that is padding get out = 0, lse = -infinity.
+ * What a query does not see has no influence on its result, whatever it holds; rows at and beyond a
+ * sequence's length are not read at all.
+ * Accuracy: products of the cache's values as they stand (a quantised row's parameters are applied in
+ * fp32), fp32 sums; probabilities enter the second product with 16 or more bits.
+ */
+typedef struct {
+  int32_t Hq;            /* query heads, a multiple of Hkv; head h reads KV head h / (Hq / Hkv)     */
+  int32_t T;             /* 1 <= T <= 1024                                                          */
+  int32_t dtype;         /* of q and out: the cache's own type, or BF16 / F16 on a quantised one    */
+  float softmax_scale;   /* 0 means 1 / sqrt(D)                                                     */
+  int64_t q_stride[3];   /* elements between consecutive sequences, heads and tokens of q; all zero: */
+  int64_t out_stride[3]; /* packed [B, Hq, T, D].  Multiples of 16 bytes.  out: the same             */
+  const uint64_t* mask;  /* NULL, or [B, T, ceil(T / 64)]                                           */
+  int64_t mask_stride;   /* words between consecutive sequences' masks; 0: one mask for all         */
+  const int32_t* n_new;  /* NULL, or [B] (see above)                                                */
+  const int32_t* blocks; /* NULL, or [B, Hkv, T, n_list] as kvcrush_block_select writes it: query t */
+                         /* sees only positions of the listed blocks of `unit` tokens.  Ascending;  */
+                         /* an entry that is negative, beyond the sequence or not larger than the   */
+                         /* one before it counts for nothing                                        */
+  int32_t n_list;        /* entries per list (blocks only)                                          */
+  int32_t unit;          /* tokens per listed block, 1 <= unit (blocks only)                        */
+} kvcrush_attend_args;
+
+/* Size limits: B * Hkv <= 65535, n_list * unit < 2^30.  lse may be NULL.  The order of summation depends on
+ * the arguments' sizes only: equal calls give equal bits. */
+size_t kvcrush_attend_workspace(const kvcrush_cache* cache, const kvcrush_attend_args* args);
+kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcrush_attend_args* args, const void* q, void* out,
+                              float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Bounds of the keys of each block of `unit` tokens: with lo_d, hi_d the least and greatest value at d of
+ * its keys (as kvcrush_cache_read gives them in fp32) and a = max(|lo|, |hi|),
+ *   bounds [B, Hkv, Nb, 2, D] int8   lo * inv, hi * inv rounded (ties to even), inv = 127 / a
+ *   scales [B, Hkv, Nb]              a / 127           (a < 2^-100, or a block without tokens: zeros)
+ * Nb = ceil(capacity / unit).  Only the blocks that hold one of the last T tokens (of the n real ones, with
+ * n_new) are computed, the others stay as they are; T = 0: every block of the sequence.  Keys are assumed
+ * finite.
+ * Size limits: unit <= 1024, B * Hkv <= 65535. */
+kvcrush_status kvcrush_block_bounds(const kvcrush_cache* cache, int32_t unit, int32_t T, const int32_t* n_new,
+                                    int8_t* bounds, float* scales, void* hip_stream);
+
+/* For each query and KV head the blocks that are worth attending to.  With q8 the query head's values in
+ * 8 bits (a = max |q|, q * (127 / a) rounded, a / 127 its scale), a block's score for that head is
+ *   ((sum_d max(q8_d, 0) * hi_d + min(q8_d, 0) * lo_d) * block scale) * head scale,
+ * an integer and two fp32 products: about the largest logit that a key of the block can have.  The heads of a
+ * KV group share the largest of their scores.  The first n_sink and last n_recent blocks of the sequence
+ * are always taken, the others by score, ties to the lower block.
+ *   bounds, scales  as kvcrush_block_bounds leaves them
+ *   blocks  [B, Hkv, T, n_select] int32: ascending; -1 where the sequence has no more blocks, and for padding
+ * Of args only Hq, T, dtype, q_stride and n_new are read (dtype may be any of q's types on any cache).
+ * Size limits: ceil(S / unit) <= 32768, Hq / Hkv <= 1024, B * Hkv <= 65535; 0 <= n_sink + n_recent <= n_select. */
+size_t kvcrush_block_select_workspace(const kvcrush_cache* cache, const kvcrush_attend_args* args, int32_t unit,
+                                      int32_t n_select);
+kvcrush_status kvcrush_block_select(const kvcrush_cache* cache, const kvcrush_attend_args* args, int32_t unit,
+                                    int32_t n_select, int32_t n_sink, int32_t n_recent, const void* q,
+                                    const int8_t* bounds, const float* scales, int32_t* blocks, void* workspace,
+                                    size_t workspace_bytes, void* hip_stream);
+
 const char* kvcrush_status_string(kvcrush_status status);
 
-/* Library version: 100 * minor + 10 * patch (120 = 0.1.2); changes whenever a struct or
+/* Library version: 100 * minor + 10 * patch (130 = 0.1.3); changes whenever a struct or
  * a signature of this header changes. */
 int32_t kvcrush_version(void);
 

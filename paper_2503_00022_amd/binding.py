@@ -15,6 +15,7 @@ _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libkvcrush.so")
 
 F32, BF16, F16 = 0, 1, 2
+E4M3, I8, I4 = 3, 4, 5     # kvcrush_format: cache rows in 8 or 4 bits
 ANCHORS = {"random": 0, "mean": 1, "alternating": 2, "explicit": 3}
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = range(5)
 
@@ -23,7 +24,8 @@ EXPORTS = (
     "kvcrush_pool_scores",
     "kvcrush_select_workspace", "kvcrush_select", "kvcrush_select_static", "kvcrush_compact", "kvcrush_scores_append_workspace",
     "kvcrush_scores_append", "kvcrush_decode_step", "kvcrush_compact_cache", "kvcrush_compact_block_table", "kvcrush_status_string",
-    "kvcrush_version",
+    "kvcrush_cache_write", "kvcrush_cache_read", "kvcrush_attend_workspace", "kvcrush_attend", "kvcrush_block_bounds",
+    "kvcrush_block_select_workspace", "kvcrush_block_select", "kvcrush_version",
 )
 
 
@@ -44,6 +46,19 @@ class SelectArgs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hs", "S", "budget", "n_important", "bit_topk", "anchor",
                                                  "score_stride", "n_sink", "n_recent", "unit")] + [
         ("anchor_seed", ctypes.c_uint64), ("anchor_bits", ctypes.c_void_p)]
+
+
+class Cache(ctypes.Structure):
+    """kvcrush_cache; made by make_cache, which also keeps the tensors that it points to."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hkv", "S", "D", "capacity", "format", "block_size", "n_blocks")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_param", "v_param", "lengths", "block_table")]
+
+
+class AttendArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("Hq", "T", "dtype")] + [
+        ("softmax_scale", ctypes.c_float), ("q_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3),
+        ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64), ("n_new", ctypes.c_void_p), ("blocks", ctypes.c_void_p),
+        ("n_list", ctypes.c_int32), ("unit", ctypes.c_int32)]
 
 
 _lib = None
@@ -87,6 +102,21 @@ def load() -> ctypes.CDLL:
         L.kvcrush_compact_cache.restype = ctypes.c_int
         L.kvcrush_compact_block_table.argtypes = [i32] * 4 + [vp] * 4
         L.kvcrush_compact_block_table.restype = ctypes.c_int
+        cache, attend, strides = ctypes.POINTER(Cache), ctypes.POINTER(AttendArgs), ctypes.POINTER(ctypes.c_int64)
+        L.kvcrush_cache_write.argtypes = [cache, i32, i32, vp, vp, strides, strides, vp, vp]
+        L.kvcrush_cache_write.restype = ctypes.c_int
+        L.kvcrush_cache_read.argtypes = [cache, i32, vp, i32, vp, vp, vp]
+        L.kvcrush_cache_read.restype = ctypes.c_int
+        L.kvcrush_attend_workspace.argtypes = [cache, attend]
+        L.kvcrush_attend_workspace.restype = sz
+        L.kvcrush_attend.argtypes = [cache, attend, vp, vp, vp, vp, sz, vp]
+        L.kvcrush_attend.restype = ctypes.c_int
+        L.kvcrush_block_bounds.argtypes = [cache, i32, i32, vp, vp, vp, vp]
+        L.kvcrush_block_bounds.restype = ctypes.c_int
+        L.kvcrush_block_select_workspace.argtypes = [cache, attend, i32, i32]
+        L.kvcrush_block_select_workspace.restype = sz
+        L.kvcrush_block_select.argtypes = [cache, attend, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.kvcrush_block_select.restype = ctypes.c_int
         L.kvcrush_status_string.argtypes = [ctypes.c_int]
         L.kvcrush_status_string.restype = ctypes.c_char_p
         L.kvcrush_version.restype = i32
@@ -424,6 +454,280 @@ def kvcrush_compact_block_table(idx, block_table, block_size: int, out=None, str
                                             _ptr(block_table), _ptr(_dev(out, "out")), _stream(stream))
     _check(st, "kvcrush_compact_block_table")
     return out
+
+
+# ------------------------------------------------------------------------------------------- using the cache
+_FORMATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3, torch.int8: I8,
+            torch.uint8: I4}
+CODES = {"e4m3": torch.float8_e4m3fn, "i8": torch.int8, "i4": torch.uint8}   # element types of quantised caches
+
+
+def make_cache(k, v, S: int, k_param=None, v_param=None, lengths=None, block_table=None) -> Cache:
+    """Describes a layer's KV cache: k, v dense [B,Hkv,capacity,D], or with block_table int32 [B,n] pools
+    [n_blocks,block_size,Hkv,D].  Their element type is the format: float32, bfloat16, float16 (no parameters), or
+    float8_e4m3fn, int8 and uint8 (4-bit pairs, D / 2 bytes a row) with k_param, v_param: float32, one number a row
+    ([B,Hkv,capacity] or [n_blocks,block_size,Hkv]; 4 bits: two, [..,2]).
+    S: valid tokens of every sequence; with lengths, int32 [B] on the GPU, their upper bound.
+    The tensors are kept alive by the result; `cache.S` may be assigned as the cache grows."""
+    for name, t in (("k", k), ("v", v)):
+        _dev(t, name)
+    if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or k.dtype not in _FORMATS:
+        raise ValueError("k and v must be 4-dimensional tensors of one shape and one of the cache's element types")
+    fmt = _FORMATS[k.dtype]
+    D = k.shape[3] * (2 if fmt == I4 else 1)
+    rows = tuple(k.shape[:3])
+    if fmt in (E4M3, I8, I4):
+        for name, t in (("k_param", k_param), ("v_param", v_param)):
+            if t is None or t.dtype != torch.float32 or tuple(_dev(t, name).shape) != (rows + (2,) if fmt == I4 else rows):
+                raise ValueError(f"{name} must be float32 {list(rows + (2,) if fmt == I4 else rows)}")
+    elif k_param is not None or v_param is not None:
+        raise ValueError("only quantised caches have parameters")
+    if block_table is None:
+        B, Hkv, capacity, block_size, n_blocks = *rows, 0, 0
+    else:
+        n_blocks, block_size, Hkv = rows
+        if block_table.dtype != torch.int32 or _dev(block_table, "block_table").dim() != 2:
+            raise ValueError("block_table must be int32 [B,n]")
+        B, capacity = block_table.shape[0], block_table.shape[1] * block_size
+    if lengths is not None and (lengths.dtype != torch.int32 or tuple(_dev(lengths, "lengths").shape) != (B,)):
+        raise ValueError("lengths must be int32 [B]")
+    tensors = (k, v, k_param, v_param, lengths, block_table)
+    if any(t is not None and t.device != k.device for t in tensors):
+        raise ValueError("the cache's tensors must live on one device")
+    cache = Cache(B, Hkv, int(S), D, capacity, fmt, block_size, n_blocks, *(None if t is None else t.data_ptr() for t in tensors))
+    cache.tensors, cache.device, cache.dtype = tensors, k.device, k.dtype
+    return cache
+
+
+class _On:
+    """The device of a call's tensors as the current one, and the stream of the call: where tensors made for it are in use."""
+
+    def __init__(self, device, stream):
+        self.index = device.index
+        self.back = torch.cuda.current_device()
+        self.stream = stream
+
+    def __enter__(self):
+        if self.index != self.back:
+            torch.cuda.set_device(self.index)
+        return _stream(self.stream)
+
+    def __exit__(self, *_):
+        if self.index != self.back:
+            torch.cuda.set_device(self.back)
+
+    def used(self, *made):
+        """Tensors made for this call under the current stream that another one uses."""
+        if self.stream is not None:
+            for t in made:
+                t.record_stream(self.stream)
+
+
+def _same_device(cache, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != cache.device:
+            raise ValueError(f"{name} must live on the cache's device")
+
+
+def _strides(t):
+    """Element strides of [B,H,T,D] (sequence, head, token); an axis of one element has any, so its packed one is given."""
+    if t.is_contiguous():
+        return None
+    B, H, T, D = t.shape
+    st = t.stride()
+    return (ctypes.c_int64 * 3)(st[0] if B > 1 else H * T * D, st[1] if H > 1 else T * D, st[2] if T > 1 else D)
+
+
+def _count(t, cache, name):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(_dev(t, name).shape) != (cache.B,):
+        raise ValueError(f"{name} must be int32 [B]")
+    return t.data_ptr()
+
+
+def kvcrush_cache_write(cache: Cache, k_new, v_new, n_new=None, stream=None):
+    """k_new, v_new [B,Hkv,T,D] (any strides, D contiguous) become the last T tokens of their sequences: the cache's
+    lengths count them already.  n_new int32 [B]: only the first n_new[b] of sequence b's are real.  Quantised caches
+    take float32, bfloat16 and float16, the others their own type."""
+    _dev_rows(k_new, "k_new"), _dev_rows(v_new, "v_new")
+    T = k_new.shape[2]
+    if v_new.shape != k_new.shape or v_new.dtype != k_new.dtype or tuple(k_new.shape) != (cache.B, cache.Hkv, T, cache.D):
+        raise ValueError("k_new and v_new must be [B,Hkv,T,D] tensors of one type that fit the cache")
+    _same_device(cache, k_new=k_new, v_new=v_new, n_new=n_new)
+    with _On(cache.device, stream) as s:
+        st = load().kvcrush_cache_write(ctypes.byref(cache), T, _dtype_code(k_new), k_new.data_ptr(), v_new.data_ptr(),
+                                        _strides(k_new), _strides(v_new), _count(n_new, cache, "n_new"), s)
+    _check(st, "kvcrush_cache_write")
+
+
+def kvcrush_cache_read(cache: Cache, idx=None, n=None, dtype=None, k_out=None, v_out=None, stream=None):
+    """The cache's rows as values: of the positions idx int32 [B,n], or of the first n (default: cache.S) tokens.
+    -> (k, v) [B,Hkv,n,D] of `dtype` (default: k_out's; the cache's own type; bfloat16 of quantised ones).  Rows that a
+    sequence does not have stay as they are in k_out and v_out; in tensors made here they are zero."""
+    if idx is not None:
+        if idx.dtype != torch.int32 or _dev(idx, "idx").dim() != 2 or idx.shape[0] != cache.B:
+            raise ValueError("idx must be int32 [B,n]")
+        n = idx.shape[1]
+    elif n is None:
+        n = cache.S
+    shape = (cache.B, cache.Hkv, int(n), cache.D)
+    if dtype is None:
+        dtype = k_out.dtype if k_out is not None else cache.dtype if cache.dtype not in CODES.values() else torch.bfloat16
+    on, made = _On(cache.device, stream), []
+    with on as s:
+        if k_out is None or v_out is None:
+            new = torch.zeros if cache.lengths or idx is None and n > cache.S else torch.empty
+            made = [new(shape, dtype=dtype, device=cache.device) for t in (k_out, v_out) if t is None]
+            if stream is not None and new is torch.zeros:   # (the zeros are written under the current stream)
+                stream.wait_stream(torch.cuda.current_stream())
+            k_out, v_out = (made[0] if k_out is None else k_out), (made[-1] if v_out is None else v_out)
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            if tuple(_dev(t, name).shape) != shape or t.dtype != dtype:
+                raise ValueError(f"{name} must be {dtype} {list(shape)}")
+        _same_device(cache, k_out=k_out, v_out=v_out, idx=idx)
+        st = load().kvcrush_cache_read(ctypes.byref(cache), n, _ptr(idx), _dtype_code(k_out), k_out.data_ptr(), v_out.data_ptr(), s)
+        on.used(*made)
+    _check(st, "kvcrush_cache_read")
+    return k_out, v_out
+
+
+def _attend_sizes(cache, Hq, T, dtype, scale=0.0, n_list=0, unit=0):
+    return AttendArgs(Hq, T, _FORMATS[dtype], float(scale), blocks=16 if n_list else None, n_list=n_list, unit=unit)
+
+
+def kvcrush_attend_workspace(cache: Cache, Hq: int, T: int, dtype, n_list=0, unit=0) -> int:
+    """Bytes of scratch memory that kvcrush_attend needs for queries [B,Hq,T,D] of `dtype` (with lists: of n_list blocks
+    of `unit` tokens) on this cache, its S and capacity being what they are now; a larger S needs no less."""
+    return int(load().kvcrush_attend_workspace(ctypes.byref(cache), ctypes.byref(_attend_sizes(cache, Hq, T, dtype, 0.0, n_list, unit))))
+
+
+def _queries(cache, q):
+    _dev_rows(q, "q")
+    B, Hq, T, D = q.shape
+    if B != cache.B or D != cache.D or q.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+        raise ValueError("q must be a float32, bfloat16 or float16 [B,Hq,T,D] that fits the cache")
+    args = AttendArgs(Hq, T, _FORMATS[q.dtype])
+    st = _strides(q)
+    if st is not None:
+        args.q_stride = st
+    return args
+
+
+def kvcrush_attend(cache: Cache, q, mask=None, n_new=None, blocks=None, unit=0, scale=0.0, out=None, lse=None, workspace=None,
+                   stream=None):
+    """The newest T tokens, whose rows are in the cache, attend to it: q [B,Hq,T,D] (any strides, D contiguous) ->
+    (out like q, lse float32 [B,Hq,T], the rows' natural log-sum-exps).
+    mask: int64 words [B,T,ceil(T/64)], or [T,ceil(T/64)] for all sequences: bit j % 64 of word j / 64 of row t lets new
+    token t see new token j; without it, those up to itself.  All tokens before the new ones are seen.
+    n_new int32 [B]: only the first n_new[b] of the T tokens are real.
+    blocks int32 [B,Hkv,T,n] (kvcrush_block_select): query t sees only these blocks of `unit` tokens."""
+    args = _queries(cache, q)
+    B, Hq, T, D = q.shape
+    args.softmax_scale = float(scale)
+    if mask is not None:
+        words = (T + 63) // 64
+        if mask.dtype != torch.int64 or tuple(_dev(mask, "mask").shape) not in ((B, T, words), (T, words)):
+            raise ValueError("mask must be int64 [B,T,ceil(T/64)] or [T,ceil(T/64)]")
+        args.mask, args.mask_stride = mask.data_ptr(), T * words if mask.dim() == 3 else 0
+    if blocks is not None:
+        if blocks.dtype != torch.int32 or _dev(blocks, "blocks").dim() != 4 or tuple(blocks.shape[:3]) != (B, cache.Hkv, T):
+            raise ValueError("blocks must be int32 [B,Hkv,T,n]")
+        args.blocks, args.n_list, args.unit = blocks.data_ptr(), blocks.shape[3], int(unit)
+    args.n_new = _count(n_new, cache, "n_new")
+    _same_device(cache, q=q, mask=mask, n_new=n_new, blocks=blocks, out=out, lse=lse, workspace=workspace)
+    L, on, made = load(), _On(cache.device, stream), []
+    with on as s:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=cache.device)
+            made.append(out)
+        else:
+            if tuple(_dev_rows(out, "out").shape) != tuple(q.shape) or out.dtype != q.dtype:
+                raise ValueError("out must have q's shape and type")
+            st = _strides(out)
+            if st is not None:
+                args.out_stride = st
+        if lse is None:
+            lse = torch.empty(B, Hq, T, dtype=torch.float32, device=cache.device)
+            made.append(lse)
+        elif lse.dtype != torch.float32 or tuple(_dev(lse, "lse").shape) != (B, Hq, T):
+            raise ValueError("lse must be float32 [B,Hq,T]")
+        if workspace is None:
+            workspace = torch.empty(max(int(L.kvcrush_attend_workspace(ctypes.byref(cache), ctypes.byref(args))), 16),
+                                    dtype=torch.uint8, device=cache.device)
+            made.append(workspace)
+        st = L.kvcrush_attend(ctypes.byref(cache), ctypes.byref(args), q.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), s)
+        on.used(*made)
+    _check(st, "kvcrush_attend")
+    return out, lse
+
+
+def kvcrush_block_bounds(cache: Cache, unit: int, bounds=None, scales=None, T=0, n_new=None, stream=None):
+    """8-bit bounds of the keys of every block of `unit` tokens: (bounds int8 [B,Hkv,Nb,2,D], scales float32 [B,Hkv,Nb]),
+    Nb = ceil(capacity / unit).  T > 0 refreshes, in bounds and scales given, the blocks of the last T tokens (of the
+    n_new[b] real ones) only."""
+    if unit < 1:
+        raise ValueError("unit must be positive")
+    nb = (cache.capacity + unit - 1) // unit
+    if (bounds is None) != (scales is None) or (bounds is None and T):
+        raise ValueError("bounds and scales come together, and are needed to refresh blocks of them")
+    _same_device(cache, bounds=bounds, scales=scales, n_new=n_new)
+    on, made = _On(cache.device, stream), []
+    with on as s:
+        if bounds is None:
+            made = [torch.zeros(cache.B, cache.Hkv, nb, 2, cache.D, dtype=torch.int8, device=cache.device),
+                    torch.zeros(cache.B, cache.Hkv, nb, dtype=torch.float32, device=cache.device)]
+            bounds, scales = made
+            if stream is not None:
+                stream.wait_stream(torch.cuda.current_stream())
+        if bounds.dtype != torch.int8 or tuple(_dev(bounds, "bounds").shape) != (cache.B, cache.Hkv, nb, 2, cache.D):
+            raise ValueError("bounds must be int8 [B,Hkv,ceil(capacity/unit),2,D]")
+        if scales.dtype != torch.float32 or tuple(_dev(scales, "scales").shape) != (cache.B, cache.Hkv, nb):
+            raise ValueError("scales must be float32 [B,Hkv,ceil(capacity/unit)]")
+        st = load().kvcrush_block_bounds(ctypes.byref(cache), unit, T, _count(n_new, cache, "n_new"), bounds.data_ptr(),
+                                         scales.data_ptr(), s)
+        on.used(*made)
+    _check(st, "kvcrush_block_bounds")
+    return bounds, scales
+
+
+def kvcrush_block_select_workspace(cache: Cache, Hq: int, T: int, dtype, unit: int, n_select: int) -> int:
+    return int(load().kvcrush_block_select_workspace(ctypes.byref(cache), ctypes.byref(_attend_sizes(cache, Hq, T, dtype)), unit,
+                                                     n_select))
+
+
+def kvcrush_block_select(cache: Cache, q, bounds, scales, unit: int, n_select: int, n_sink=1, n_recent=1, n_new=None, blocks=None,
+                         workspace=None, stream=None):
+    """For each query of q [B,Hq,T,D] and each KV head the n_select blocks to attend to: int32 [B,Hkv,T,n_select],
+    ascending, -1 behind the last.  The first n_sink and last n_recent blocks of the sequence are among them, the others
+    are those of the largest scores by kvcrush_block_bounds' bounds and scales."""
+    args = _queries(cache, q)
+    B, Hq, T, D = q.shape
+    if unit < 1:
+        raise ValueError("unit must be positive")
+    nb = (cache.capacity + unit - 1) // unit
+    if bounds.dtype != torch.int8 or tuple(_dev(bounds, "bounds").shape) != (B, cache.Hkv, nb, 2, D)             or scales.dtype != torch.float32 or tuple(_dev(scales, "scales").shape) != (B, cache.Hkv, nb):
+        raise ValueError("bounds int8 [B,Hkv,ceil(capacity/unit),2,D] and scales float32 [B,Hkv,ceil(capacity/unit)]")
+    args.n_new = _count(n_new, cache, "n_new")
+    _same_device(cache, q=q, bounds=bounds, scales=scales, n_new=n_new, blocks=blocks, workspace=workspace)
+    L, on, made = load(), _On(cache.device, stream), []
+    with on as s:
+        if blocks is None:
+            blocks = torch.empty(B, cache.Hkv, T, max(int(n_select), 0), dtype=torch.int32, device=cache.device)
+            made.append(blocks)
+        elif blocks.dtype != torch.int32 or tuple(_dev(blocks, "blocks").shape) != (B, cache.Hkv, T, n_select):
+            raise ValueError("blocks must be int32 [B,Hkv,T,n_select]")
+        if workspace is None:
+            need = int(L.kvcrush_block_select_workspace(ctypes.byref(cache), ctypes.byref(args), unit, n_select))
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
+            made.append(workspace)
+        st = L.kvcrush_block_select(ctypes.byref(cache), ctypes.byref(args), unit, n_select, n_sink, n_recent, q.data_ptr(),
+                                    bounds.data_ptr(), scales.data_ptr(), blocks.data_ptr(), workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), s)
+        on.used(*made)
+    _check(st, "kvcrush_block_select")
+    return blocks
 
 
 def kvcrush_version() -> int:
