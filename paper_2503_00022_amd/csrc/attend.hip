@@ -2,14 +2,16 @@
 // own type or quantised, over all of it or over listed blocks.
 //
 // The queries of all heads of a KV group and of all new tokens are the rows that one key serves: R = T * G of
-// them.  A wave takes 32 keys at a time and 32 or 64 of those rows (NC = 1, 2):
-//   S^T = K Q^T      keys x rows, 32x32 matrix instructions: a lane holds one row's logits of 16 keys
-//   softmax          running maximum and sum per row in registers
+// them.  A wave takes kTile keys at a time and 16 NC of those rows (NC = 1, 2, 4):
+//   S^T = K Q^T      keys x rows, 16x16 matrix instructions: a lane holds one row's logits, of every fourth group of
+//                    four keys
+//   softmax          one reference exponent and one sum per row in registers
 //   O^T += V^T P^T   the probabilities are already laid out as the second product's operand; V is read
 //                    transposed from LDS (ds_read_b64_tr)
-// Waves share nothing until their keys are done: each copies its own tiles into its own part of the LDS, and
-// the workgroup's waves merge their rows at the end.  The keys of a sequence are cut over workgroups so that the
-// chip is full; the pieces' results are merged by a second kernel.
+// Bound by reading K and V (4 R flops for a value read).  Waves share nothing until their keys are done: each copies
+// its own tiles asynchronously into its own part of the LDS, kStages of them in flight, and waits for nobody; at the
+// end the workgroup's waves add up their rows.  The keys of a sequence are cut over workgroups so that the chip is
+// full; the pieces' results are merged by a second kernel.
 #include <algorithm>
 #include <cmath>
 
@@ -19,30 +21,29 @@
 namespace {
 
 using namespace kvc::cache;
-using kvc::tiles::f32x16;
 using kvc::tiles::kLn2;
 using kvc::tiles::kNegBig;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
-constexpr float kMasked = -3.0e38f;  // below every running maximum (>= kNegBig) by more than any exponent
-constexpr int kTile = 32;            // keys of a tile
-constexpr int kAhead = 1024;         // keys whose places a wave looks up at once
+constexpr int kAhead = 512;         // keys whose places a wave looks up at once
 
 struct AttendParams {
   View c;
   const char* q;
   char* out;
   float* lse;
-  float* part_o;   // workspace [B * Hkv * rows][n_split][D], rows = G * T
-  float2* part_ml;  // workspace [B * Hkv * rows][n_split]
+  float* part_o;   // workspace [B * Hq * T][n_split][D]
+  float2* part_ml;  // workspace [B * Hq * T][n_split]
   const uint64_t* mask;
   const int32_t* n_new;
   const int32_t* blocks;
   int64_t q_stride[3], out_stride[3];  // elements
   int64_t mask_stride;
   int Hq, G, T, n_split, n_list, unit, mask_words, q_dtype;
+  int row_tiles, groups;  // workgroups that share a sequence's piece; pieces of all sequences and KV heads
   float scale_log2;
 };
 
@@ -53,46 +54,53 @@ struct Fmt {
   static constexpr int kBits = format_bits(FORMAT);
   static constexpr int kRow = D * kBits / 8;       // bytes of a row
   static constexpr int kChunks = kRow / 16;        // 16-byte chunks of a row
+  // Keys of a tile: 32 are one step of the second product; transposed reads of 4-bit values bring 64 at a time.
+  static constexpr int kTile = kBits == 32 ? 16 : kBits == 4 ? 64 : 32;
+  static constexpr int kSub = kTile / 16;          // groups of 16 keys
   static constexpr int kTileBytes = kTile * kRow;
-  static constexpr int kLoads = kTileBytes / 1024;  // wave instructions that copy a tile
+  static constexpr int kLoads = kTileBytes / 1024;  // wave instructions that copy a tile of K (or V)
   static constexpr int kParam = kQuant ? (FORMAT == KVCRUSH_I4 ? 2 : 1) : 0;  // floats beside a row
-  static constexpr int kParamBytes = 2 * kTile * 4 * kParam;                  // K's, then V's, of a tile
-  static constexpr int kStage = 2 * kTileBytes + kParamBytes;
-  static constexpr int kWaves = kRow == 512 ? 2 : 4;
-  static constexpr int kSteps = D / 16;            // matrix steps of 16 values along D (16-bit operands)
-  static constexpr int kDTiles = D / 32;
+  static constexpr int kParamLoads = kParam * 2 * kTile / 64;                 // of 4 bytes a lane
+  static constexpr int kStage = 2 * kTileBytes + kParamLoads * 256;
+  static constexpr int kStages = 2;
+  // Eight waves where LDS and registers have room for them: two to a SIMD, so that one's matrix instructions run beside
+  // the other's arithmetic.
+  static constexpr int waves(int NC) {
+    return NC == 4 || (NC == 2 && kBits == 4) || kStage * kStages * 8 + 8 * kAhead * 4 > kvc::kLdsPerWorkgroup ? 4 : 8;
+  }
+  static constexpr int kSteps = D / 32;            // matrix steps of 32 values along D (16-bit operands)
+  static constexpr int kDTiles = D / 16;
   static_assert(kTileBytes % 1024 == 0, "whole wave instructions");
 
-  // XOR on a 16-byte chunk's place in its 256-byte line.  K is read one chunk a lane, neighbouring lanes
-  // neighbouring rows; V in pieces of 16 values x 4, 8 or 16 rows (transposed), which must not share banks.
-  __device__ static int k_xor(int line) { return line & 15; }
-  __device__ static int v_xor(int line) {
-    if constexpr (kBits == 32) return kRow == 512 ? ((line >> 3) & 1) << 3 : ((line >> 2) & 1) << 3;
-    if constexpr (kBits == 16) return kRow == 256 ? ((line & 3) << 2) | ((line >> 2) & 3) : (line & 1) << 2;
-    if constexpr (kBits == 8) return kRow == 128 ? ((line & 1) | ((line >> 1) & 2)) << 1 : ((line >> 1) & 1) << 1;
-    return kRow == 64 ? (line >> 1) & 3 : (line & 1) | ((line & 2) << 2);
+  // XOR on a 16-byte chunk's place in its 256-byte line of the tile's image, by the line's number.  Two reads must find
+  // their pieces in different banks: K's, one chunk of 16 neighbouring rows; V's, transposed, 8 values (4-bit: 16) of
+  // 4 values' width of rows that differ in bits 0, 1, 2 (8-bit: and 4; 4-bit: 4 and 5).
+  __device__ static int swizzle(int line) {
+    const int l0 = line & 1, l1 = (line >> 1) & 1, l2 = (line >> 2) & 1, l3 = (line >> 3) & 1;
+    if constexpr (kBits == 32) return kRow == 512 ? (line >> 1) & 15 : line & 15;
+    if constexpr (kBits == 16) return kRow == 256 ? ((line & 7) << 1) | l3 : ((line & 3) << 1) | l2;
+    if constexpr (kBits == 8) return kRow == 128 ? l0 | (l1 << 1) | ((l2 ^ l3) << 2) : l0 | ((l1 ^ l2) << 1);
+    return kRow == 64 ? (l0 ^ l2) | ((l1 ^ l3) << 1) : l0 ^ l1;
   }
-  template <bool V>
-  __device__ static int chunk_at(int row, int chunk) {  // byte offset in the tile's image
+  __device__ static int chunk_at(int row, int chunk) {  // byte offset in the image
     const int q = row * kChunks + chunk, line = q >> 4;
-    return (line << 8) | (((q & 15) ^ (V ? v_xor(line) : k_xor(line))) << 4);
+    return (line << 8) | (((q & 15) ^ swizzle(line)) << 4);
   }
   // The row and chunk whose bytes lie at physical chunk `p` of the image.
-  template <bool V>
   __device__ static void chunk_of(int p, int& row, int& chunk) {
-    const int line = p >> 4, q = line * 16 + ((p & 15) ^ (V ? v_xor(line) : k_xor(line)));
+    const int line = p >> 4, q = line * 16 + ((p & 15) ^ swizzle(line));
     row = q / kChunks;
     chunk = q % kChunks;
   }
 };
 
-// C += A B^T for one step of 16 values along the inner axis; operands are halves unless the cache is bfloat16.
+// C += A B^T for one step of 32 values along the inner axis; operands are halves unless the cache is bfloat16.
 template <int FORMAT>
-__device__ __forceinline__ void mma16(f32x16& c, const u32x4& a, const u32x4& b) {
+__device__ __forceinline__ void mma(f32x4& c, const u32x4& a, const u32x4& b) {
   if constexpr (FORMAT == KVCRUSH_BF16)
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else
-    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 __device__ __forceinline__ u32x2 read_tr16(const char* p) {
@@ -105,53 +113,79 @@ __device__ __forceinline__ u32x2 read_tr4(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) i32x2*)p));
 }
 
-__device__ __forceinline__ int acc_key(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
+// The largest of the four lanes of a row (lane, lane ^ 16, lane ^ 32, lane ^ 48), and their sum.
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
 
-// K fragments of the 32 keys for 16-byte chunk j of this lane's half of a row: kSub matrix steps.
+// Keys: register r of group u of lane group g = lane / 16 holds key 16 u + 4 g + r; element e of a step of 32 keys is
+// register e % 4 of group e / 4.
+__device__ __forceinline__ int step_key(int g, int e) { return 16 * (e >> 2) + 4 * g + (e & 3); }
+
+// K's operands for 16 keys: all matrix steps.  A lane takes 16-byte chunks 4 j + g of its key's row (the order of the
+// inner axis is free; the queries follow it).
 template <class F>
-struct KFrag {
-  static constexpr int kSub = F::kBits == 32 ? 1 : 16 / F::kBits;  // steps that one chunk feeds
-  u32x4 f[kSub];
-  __device__ __forceinline__ void load(const char* tile, int lane, int j) {
-    const u32x4 w = *(const u32x4*)(tile + F::template chunk_at<false>(lane & 31, (lane >> 5) * (F::kChunks / 2) + j));
-    if constexpr (F::kBits >= 16) {
-      f[0] = w;
-    } else if constexpr (F::kBits == 8) {
+__device__ __forceinline__ void k_frags(const char* tile, int lane, int u, u32x4 (&f)[F::kBits == 32 ? F::D / 16 : F::kSteps]) {
+  const int row = 16 * u + (lane & 15), g = lane >> 4;
+  if constexpr (F::kBits >= 16) {
+#pragma unroll
+    for (int j = 0; j < F::kChunks / 4; ++j) f[j] = *(const u32x4*)(tile + F::chunk_at(row, 4 * j + g));
+  } else if constexpr (F::kBits == 8) {
+#pragma unroll
+    for (int j = 0; j < F::kChunks / 4; ++j) {
+      const u32x4 w = *(const u32x4*)(tile + F::chunk_at(row, 4 * j + g));
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const u32x2 a = codes4_to_f16<F::FORMAT>(w[2 * i]), b = codes4_to_f16<F::FORMAT>(w[2 * i + 1]);
-        f[i] = u32x4{a[0], a[1], b[0], b[1]};
+        f[2 * j + i] = u32x4{a[0], a[1], b[0], b[1]};
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = codes8_to_f16(w[i]);
     }
+  } else if constexpr (F::kChunks == 4) {
+    const u32x4 w = *(const u32x4*)(tile + F::chunk_at(row, g));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = codes8_to_f16(w[i]);
+  } else {
+    const u32x2 w = *(const u32x2*)(tile + F::chunk_at(row, g >> 1) + (g & 1) * 8);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) f[i] = codes8_to_f16(w[i]);
   }
-};
-
-// V^T fragment: lane = value d (of 32) of tile dt, the eight keys acc_key(8 * step + e, half) in order.
+}
+// First value of the eight (four of a 32-bit type) that this lane's step t of the inner axis has.
 template <class F>
-__device__ __forceinline__ u32x4 v_frag(const char* tile, int lane, int dt, int step) {
-  const int half = lane >> 5, group = (lane >> 4) & 1, i = lane & 15;
+__device__ __forceinline__ int step_value(int g, int t) {
+  if constexpr (F::kBits == 32) return (4 * t + g) * 4;
+  if constexpr (F::kBits == 16) return (4 * t + g) * 8;
+  if constexpr (F::kBits == 8) return (4 * (t >> 1) + g) * 16 + (t & 1) * 8;
+  return F::kChunks == 4 ? g * 32 + t * 8 : g * 16 + t * 8;
+}
+
+// V^T's operand of 16 values (tile dt) x 32 keys (step ks): lane = value, its eight keys step_key(g, e).
+template <class F>
+__device__ __forceinline__ u32x4 v_frag(const char* tile, int lane, int dt, int ks) {
+  const int g = lane >> 4, i = lane & 15;
   if constexpr (F::kBits == 16) {
-    const int row = 16 * step + 4 * half + (i >> 2), chunk = dt * 4 + group * 2 + ((i & 3) >> 1), off = (i & 1) * 8;
-    const u32x2 a = read_tr16(tile + F::template chunk_at<true>(row, chunk) + off);
-    const u32x2 b = read_tr16(tile + F::template chunk_at<true>(row + 8, chunk) + off);
+    const int row = 32 * ks + 4 * g + (i >> 2), chunk = dt * 2 + ((i & 3) >> 1), off = (i & 1) * 8;
+    const u32x2 a = read_tr16(tile + F::chunk_at(row, chunk) + off), b = read_tr16(tile + F::chunk_at(row + 16, chunk) + off);
     return u32x4{a[0], a[1], b[0], b[1]};
   } else {
     static_assert(F::kBits == 8, "");
-    const int row = acc_key(8 * step + (i >> 1), half);
-    const u32x2 w = read_tr8(tile + F::template chunk_at<true>(row, dt * 2 + group) + (i & 1) * 8);
+    const int row = 32 * ks + step_key(g, i >> 1);
+    const u32x2 w = read_tr8(tile + F::chunk_at(row, dt) + (i & 1) * 8);
     const u32x2 a = codes4_to_f16<F::FORMAT>(w[0]), b = codes4_to_f16<F::FORMAT>(w[1]);
     return u32x4{a[0], a[1], b[0], b[1]};
   }
 }
-// Both steps' fragments of 4-bit codes: one read.  codes8_to_f16's order is undone by the order of the rows.
+// 4-bit codes of 64 keys: one word a step.  codes8_to_f16's order is undone by the order of the rows.
 template <class F>
 __device__ __forceinline__ u32x2 v_codes4(const char* tile, int lane, int dt) {
-  const int half = lane >> 5, group = (lane >> 4) & 1, i = lane & 15, j = i & 7;
-  const int row = acc_key((i & 8) + (j < 4 ? 2 * j : 2 * j - 7), half);
-  return read_tr4(tile + F::template chunk_at<true>(row, dt) + group * 8);
+  const int g = lane >> 4, i = lane & 15, j = i & 7;
+  const int row = 32 * (i >> 3) + step_key(g, j < 4 ? 2 * j : 2 * j - 7);
+  return read_tr4(tile + F::chunk_at(row, dt >> 1) + (dt & 1) * 8);
 }
 
 template <int FORMAT>
@@ -166,7 +200,7 @@ __device__ __forceinline__ bool all_finite(uint32_t w) {  // the values in one w
 template <class F>
 __device__ __forceinline__ float tile_value(const char* tile, int key, int d) {
   const int at = d * F::kBits / 8;
-  const char* p = tile + F::template chunk_at<true>(key, at >> 4) + (at & 15);
+  const char* p = tile + F::chunk_at(key, at >> 4) + (at & 15);
   if constexpr (F::FORMAT == KVCRUSH_F32) return *(const float*)p;
   if constexpr (F::FORMAT == KVCRUSH_BF16) return __uint_as_float((uint32_t) * (const uint16_t*)p << 16);
   if constexpr (F::FORMAT == KVCRUSH_F16) return (float)*(const _Float16*)p;
@@ -174,7 +208,7 @@ __device__ __forceinline__ float tile_value(const char* tile, int key, int d) {
   return (float)as_f16x2(h[0])[0];
 }
 
-// What a query sees of one key slot: position and whether the slot exists.
+// Position of a key slot, and whether there is a token.
 struct Slots {
   const int32_t* list;  // this query's blocks, or null
   int n, unit, L;
@@ -190,50 +224,159 @@ struct Slots {
   }
 };
 
+// Asynchronous copies into LDS, 16 or 4 bytes a lane to `dst` + 16 or 4 x lane (dst uniform).  Written out, so that the
+// compiler does not wait for all of them before each LDS read that follows; whoever reads waits with wait_copies and
+// whoever overwrites what was read, with wait_reads.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(const char* from, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(dst), "v"(from) : "m0", "memory");
+}
+__device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t dst) {  // base uniform
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(off), "s"(base) : "m0", "memory");
+}
+__device__ __forceinline__ void copy4(const char* from, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(dst), "v"(from) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() {  // until at most LEFT of this wave's are under way
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Four values of a row, from its sums: out = sum / total, lse = m + log2 total.
+__device__ __forceinline__ void store_result(const AttendParams& p, int b, int head, int t, int e, float m, float total, f32x4 sum) {
+  if (p.lse && e == 0)
+    p.lse[((size_t)b * p.Hq + head) * p.T + t] = total == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(total)) * kLn2;
+  const float inv = 1.0f / total;
+  float x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = total == 0.0f ? 0.0f : sum[i] * inv;
+  const size_t at = (size_t)b * p.out_stride[0] + (size_t)head * p.out_stride[1] + (size_t)t * p.out_stride[2] + e;
+  if (p.q_dtype == KVCRUSH_F32)
+    *(f32x4*)(p.out + at * 4) = f32x4{x[0], x[1], x[2], x[3]};
+  else if (p.q_dtype == KVCRUSH_BF16)
+    *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_BF16>(x[0], x[1]), pack2<KVCRUSH_BF16>(x[2], x[3])};
+  else
+    *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_F16>(x[0], x[1]), pack2<KVCRUSH_F16>(x[2], x[3])};
+}
+
 template <class F, int NC>
-__global__ __launch_bounds__(F::kWaves * KVC_WAVE) void attend_kernel(AttendParams p) {
-  constexpr int D = F::D, FORMAT = F::FORMAT;
+__global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendParams p) {
+  constexpr int kWaves = F::waves(NC);
+  constexpr int D = F::D, FORMAT = F::FORMAT, kTile = F::kTile, U = F::kSub;
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   const int tid = threadIdx.x, lane = kvc::lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / KVC_WAVE);
-  const int half = lane >> 5, col = lane & 31;
-  const int split = blockIdx.x, bh = blockIdx.z, b = bh / p.c.Hkv, h = bh % p.c.Hkv;
+  const int g = lane >> 4, col = lane & 15;
+  // Workgroups with numbers 8 apart run on one chiplet, one after the other: the row tiles of a piece, which read the same
+  // keys, are put there side by side.
+  const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, row_tile = place % p.row_tiles;
+  const int group = place / p.row_tiles * 8 + xcd;
+  if (group >= p.groups) return;
+  const int bh = group / p.n_split, split = group - bh * p.n_split, b = bh / p.c.Hkv, h = bh - b * p.c.Hkv;
   const int L = p.c.length(b), n = new_tokens(p.n_new, b, p.T, L);
-  const int t_list = p.blocks ? (int)blockIdx.y : 0;           // with lists: the query, whose G heads are the rows
-  const int row0 = p.blocks ? 0 : (int)blockIdx.y * 32 * NC;
+  // with lists, a query's G heads are the rows
+  const int tiles_of_query = (p.G + 16 * NC - 1) / (16 * NC);
+  const int t_list = p.blocks ? row_tile / tiles_of_query : 0;
+  const int row0 = (p.blocks ? row_tile % tiles_of_query : row_tile) * 16 * NC;
   const int rows = p.blocks ? p.G : p.G * p.T;
 
   Slots slots;
   slots.list = p.blocks ? p.blocks + ((size_t)bh * p.T + t_list) * p.n_list : nullptr;
-  slots.unit = p.blocks ? p.unit : 1;
+  slots.unit = p.unit;
   slots.n = p.blocks ? (t_list < n ? p.n_list * p.unit : 0) : n > 0 ? L : 0;
   slots.L = L;
 
-  // this lane's rows
-  int t_of[NC];
-  const char* q_row[NC];
-  bool live[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int r = row0 + c * 32 + col;
-    live[c] = r < rows;
-    const int rr = live[c] ? r : rows - 1;
-    const int t = p.blocks ? t_list : rr / p.G, g = p.blocks ? rr : rr - t * p.G;
-    t_of[c] = t;
-    const int elem = format_bits(p.q_dtype) / 8;
-    q_row[c] = p.q + ((size_t)b * p.q_stride[0] + (size_t)(h * p.G + g) * p.q_stride[1] + (size_t)t * p.q_stride[2]) * elem;
-  }
+  // this wave's tiles: a contiguous piece of the workgroup's
+  const int tiles = (slots.n + kTile - 1) / kTile, per_wg = (tiles + p.n_split - 1) / p.n_split;
+  const int wg0 = min(split * per_wg, tiles), wg1 = min(wg0 + per_wg, tiles);
+  const int per_wave = (wg1 - wg0 + kWaves - 1) / kWaves;
+  const int tile0 = min(wg0 + wave * per_wave, wg1), tile1 = min(tile0 + per_wave, wg1);
 
-  // queries as the first product's other operand: in the order of the K fragments
-  constexpr int kQRegs = F::kBits == 32 ? D / 8 : F::kSteps;
+  // ---- copies of tiles into this wave's stages
+  char* own = lds_all + wave * (F::kStages * F::kStage + kAhead * 4);
+  const uint32_t own_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)own);
+  int* places = (int*)(own + F::kStages * F::kStage);  // token of each slot; bit 31: the slot has to be looked at
+  const size_t row_base = p.c.base(b, h), row_step = p.c.step();
+  const bool lookup = p.c.table || p.blocks;
+  const int first_new = L - n;
+  uint32_t looks = 0;  // bit i % 32: tile tile0 + i has such slots (lookups only)
+  uint32_t in_tile[F::kLoads];  // this lane's bytes of a tile whose rows lie one behind the other
+#pragma unroll
+  for (int j = 0; j < F::kLoads; ++j) {
+    int row, chunk;
+    F::chunk_of(j * 64 + lane, row, chunk);
+    in_tile[j] = row * F::kRow + chunk * 16;
+  }
+  constexpr int kCopies = 2 * F::kLoads + F::kParamLoads;
+  auto issue = [&](int tile) {
+    const int k0 = tile * kTile, i = tile - tile0, ahead = (i * kTile) & (kAhead - 1);
+    const uint32_t dst = own_at + (i % F::kStages) * F::kStage;
+    if (lookup && ahead == 0) {
+      const int end = min(kAhead, (tile1 - tile) * kTile);
+      for (int x = lane; x < end; x += KVC_WAVE) {
+        int pos;
+        const bool there = slots.position(k0 + x, pos);
+        places[x] = p.c.token(b, there ? pos : 0) | (!there || pos >= first_new ? (int)0x80000000 : 0);
+      }
+      kvc::wave_fence();
+    }
+    if (!lookup && k0 + kTile <= L) {
+      const size_t from = (row_base + k0) * F::kRow;
+      const char *k = kvc::tiles::wave_uniform(p.c.k + from), *v = kvc::tiles::wave_uniform(p.c.v + from);
+#pragma unroll
+      for (int j = 0; j < F::kLoads; ++j) copy16(k, in_tile[j], dst + j * 1024);
+#pragma unroll
+      for (int j = 0; j < F::kLoads; ++j) copy16(v, in_tile[j], dst + F::kTileBytes + j * 1024);
+    } else {
+#pragma unroll
+      for (int j = 0; j < F::kLoads; ++j) {
+        const int row = in_tile[j] / F::kRow;
+        const int tok = lookup ? places[ahead + row] & 0x7FFFFFFF : min(k0 + row, L - 1);
+        const size_t from = (row_base + (size_t)tok * row_step) * F::kRow + in_tile[j] % F::kRow;
+        copy16(p.c.k + from, dst + j * 1024);
+        copy16(p.c.v + from, dst + F::kTileBytes + j * 1024);
+      }
+    }
+    if constexpr (F::kQuant) {
+#pragma unroll
+      for (int j = 0; j < F::kParamLoads; ++j) {
+        // [parameter][K, V][key] floats
+        const int e = j * 64 + lane, key = e % kTile, which = (e / kTile) & 1, par = e / (2 * kTile);
+        const int tok = lookup ? places[ahead + key] & 0x7FFFFFFF : min(k0 + key, L - 1);
+        const float* src = which ? p.c.v_param : p.c.k_param;
+        copy4((const char*)(src + (row_base + (size_t)tok * row_step) * F::kParam + par), dst + 2 * F::kTileBytes + j * 256);
+      }
+    }
+    if (lookup) {
+      const bool look = __ballot(places[ahead + (lane & (kTile - 1))] < 0) != 0;
+      looks = (looks & ~(1u << (i & 31))) | (look ? 1u << (i & 31) : 0u);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < F::kStages - 1; ++i)
+    if (tile0 + i < tile1) issue(tile0 + i);
+
+  // ---- this lane's rows, and the queries as the first product's other operand
+  constexpr int kQRegs = F::kBits == 32 ? D / 16 : F::kSteps;
+  int t_of[NC];
+  bool live[NC];
   u32x4 qf[NC][kQRegs];
   float col_scale[NC], q_sum[NC];  // logit = (products) * col_scale; q_sum: the lowest value's factor
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
+    const int r = row0 + c * 16 + col;
+    live[c] = r < rows;
+    const int rr = live[c] ? r : rows - 1;
+    const int t = p.blocks ? t_list : rr / p.G, head = h * p.G + (p.blocks ? rr : rr - t * p.G);
+    t_of[c] = t;
+    const char* q = p.q + ((size_t)b * p.q_stride[0] + (size_t)head * p.q_stride[1] + (size_t)t * p.q_stride[2]) * (format_bits(p.q_dtype) / 8);
     col_scale[c] = p.scale_log2;
     q_sum[c] = 0.0f;
     if constexpr (!F::kQuant) {
 #pragma unroll
-      for (int j = 0; j < kQRegs; ++j) qf[c][j] = *(const u32x4*)(q_row[c] + (half * kQRegs + j) * 16);
+      for (int j = 0; j < kQRegs; ++j) qf[c][j] = *(const u32x4*)(q + step_value<F>(g, j) * (F::kBits / 8));
     } else {
       // Halves for every type of query: a row is scaled by the power of two that brings its largest value to
       // 2^14 .. 2^15, so that a bfloat16 value loses nothing unless it is 2^-29 of the largest.
@@ -241,19 +384,20 @@ __global__ __launch_bounds__(F::kWaves * KVC_WAVE) void attend_kernel(AttendPara
       uint32_t top = 0;
 #pragma unroll
       for (int s = 0; s < F::kSteps; ++s) {
-        const int d = half * (D / 2) + s * 8;
+        const int d = step_value<F>(g, s);
         if (p.q_dtype == KVCRUSH_BF16)
-          load8<KVCRUSH_BF16>(q_row[c] + d * 2, x[s]);
+          load8<KVCRUSH_BF16>(q + d * 2, x[s]);
         else
-          load8<KVCRUSH_F16>(q_row[c] + d * 2, x[s]);
+          load8<KVCRUSH_F16>(q + d * 2, x[s]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           top = max(top, __float_as_uint(x[s][i]) & 0x7FFFFFFFu);
           q_sum[c] += x[s][i];
         }
       }
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
       top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-      q_sum[c] += __shfl_xor(q_sum[c], 32);
+      q_sum[c] = row_sum(q_sum[c]);
       const int up = min(141 - (int)(top >> 23), 126);  // >= -114
       const float by = __builtin_amdgcn_ldexpf(1.0f, up);
       q_sum[c] *= by;
@@ -268,168 +412,148 @@ __global__ __launch_bounds__(F::kWaves * KVC_WAVE) void attend_kernel(AttendPara
     }
   }
 
-  f32x16 o[NC][F::kDTiles];
-  float m[NC], l[NC], z[NC];  // running maximum (base 2), sum of this half's keys, sum of probability x lowest value
-  float unit[NC];             // quantised: what o is to be multiplied with
+  f32x4 o[NC][F::kDTiles];
+  // Reference exponent m (base 2) of a row: o, l and z are sums of 2^(logit - m).  It need not be the largest logit: it is
+  // raised, and the sums brought to it, only when a product of probability and V's scale passes 2^8 (or, where scales are
+  // tiny, a probability passes 2^96), so that what is rounded to 16 bits lies in their range and few tiles pay for it.
+  float m[NC], l[NC], z[NC];  // l: sum of this lane's keys; z: sum of probability x lowest value
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     m[c] = kNegBig;
-    l[c] = z[c] = unit[c] = 0.0f;
+    l[c] = z[c] = 0.0f;
 #pragma unroll
-    for (int d = 0; d < F::kDTiles; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[c][d][r] = 0.0f;
+    for (int d = 0; d < F::kDTiles; ++d) o[c][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // this wave's tiles: a contiguous piece of the workgroup's
-  const int tiles = (slots.n + kTile - 1) / kTile, per_wg = (tiles + p.n_split - 1) / p.n_split;
-  const int wg0 = min(split * per_wg, tiles), wg1 = min(wg0 + per_wg, tiles);
-  const int per_wave = (wg1 - wg0 + F::kWaves - 1) / F::kWaves;
-  const int tile0 = min(wg0 + wave * per_wave, wg1), tile1 = min(tile0 + per_wave, wg1);
-
-  char* stage = lds_all + wave * (F::kStage + kAhead * 4);
-  int* places = (int*)(stage + F::kStage);  // token of each slot; bit 31: the slot has to be looked at
-  const size_t row_base = p.c.base(b, h), row_step = p.c.step();
-  const bool lookup = p.c.table || p.blocks;
-  const int first_new = L - n;
-
   for (int tile = tile0; tile < tile1; ++tile) {
-    const int k0 = tile * kTile, ahead = (tile - tile0) & (kAhead / kTile - 1);
-    if (lookup && ahead == 0) {
-      const int end = min(kAhead, (tile1 - tile) * kTile);
-      for (int i = lane; i < end; i += KVC_WAVE) {
-        int pos;
-        const bool there = slots.position(k0 + i, pos);
-        const int at = p.c.token(b, there ? pos : 0);
-        places[i] = at | (!there || pos >= first_new ? (int)0x80000000 : 0);
-      }
-      kvc::wave_fence();
+    const int k0 = tile * kTile;
+    if (tile + F::kStages - 1 < tile1) {
+      wait_reads();  // (of the stage that is filled again)
+      issue(tile + F::kStages - 1);
+      wait_copies<(F::kStages - 1) * kCopies>();
+    } else {
+      wait_copies<0>();
     }
-    // ---- the tile's rows, their parameters
-    auto row_of = [&](int key) -> size_t {
-      const int tok = lookup ? places[ahead * kTile + key] & 0x7FFFFFFF : min(k0 + key, L - 1);
-      return row_base + (size_t)tok * row_step;
-    };
+    const char* kt = own + (tile - tile0) % F::kStages * F::kStage;
+    const char* vt = kt + F::kTileBytes;
+    const float* kp = (const float*)(kt + 2 * F::kTileBytes);  // [parameter][K, V][key]
+    const float* vp = kp + kTile;
+    const bool look = lookup ? (looks >> ((tile - tile0) & 31)) & 1 : k0 + kTile > first_new;
+
+    // ---- logits, but for the row's factor
+    f32x4 s[NC][U];
 #pragma unroll
-    for (int j = 0; j < F::kLoads; ++j) {
-      int row, chunk;
-      F::template chunk_of<false>(j * 64 + lane, row, chunk);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p.c.k + row_of(row) * F::kRow + chunk * 16),
-                                       (__attribute__((address_space(3))) void*)(stage + j * 1024), 16, 0, 0);
-      F::template chunk_of<true>(j * 64 + lane, row, chunk);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p.c.v + row_of(row) * F::kRow + chunk * 16),
-                                       (__attribute__((address_space(3))) void*)(stage + F::kTileBytes + j * 1024), 16, 0, 0);
+    for (int u = 0; u < U; ++u) {
+      u32x4 kf[kQRegs];
+      k_frags<F>(kt, lane, u, kf);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < kQRegs; ++j) {
+          if constexpr (F::kBits == 32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[j][i]), __uint_as_float(qf[c][j][i]), acc, 0, 0, 0);
+          } else {
+            mma<FORMAT>(acc, kf[j], qf[c][j]);
+          }
+        }
+        s[c][u] = acc;
+      }
     }
     if constexpr (F::kQuant) {
-      const float* src = half ? p.c.v_param : p.c.k_param;
-      float* dst = (float*)(stage + 2 * F::kTileBytes) + half * kTile * F::kParam;
-      const size_t row = row_of(col);
 #pragma unroll
-      for (int i = 0; i < F::kParam; ++i) dst[i * kTile + col] = src[row * F::kParam + i];
-    }
-    bool look = lookup ? __ballot(places[ahead * kTile + col] < 0) != 0 : k0 + kTile > first_new;
-    kvc::tiles::wait_async_loads();
-    kvc::wave_fence();
-    const char *kt = stage, *vt = stage + F::kTileBytes;
-    const float* kp = (const float*)(stage + 2 * F::kTileBytes);
-    const float* vp = kp + kTile * F::kParam;
-
-    // ---- logits
-    f32x16 s[NC];
+      for (int u = 0; u < U; ++u) {
+        const f32x4 scale = *(const f32x4*)(kp + 16 * u + 4 * g);
+        f32x4 low = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (FORMAT == KVCRUSH_I4) low = *(const f32x4*)(kp + 2 * kTile + 16 * u + 4 * g);
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-    constexpr int kSub = KFrag<F>::kSub;
-#pragma unroll
-    for (int j = 0; j < F::kChunks / 2; ++j) {
-      KFrag<F> kf;
-      kf.load(kt, lane, j);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if constexpr (F::kBits == 32) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf.f[0][i]), __uint_as_float(qf[c][j][i]), s[c], 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int i = 0; i < kSub; ++i) mma16<FORMAT>(s[c], kf.f[i], qf[c][j * kSub + i]);
-        }
+          for (int r = 0; r < 4; ++r)
+            s[c][u][r] = FORMAT == KVCRUSH_I4 ? __builtin_fmaf(s[c][u][r], scale[r], low[r] * q_sum[c]) : s[c][u][r] * scale[r];
       }
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int key = acc_key(r, half);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float x = s[c][r];
-        if constexpr (FORMAT == KVCRUSH_I4)
-          x = __builtin_fmaf(x, kp[key], kp[kTile + key] * q_sum[c]);
-        else if constexpr (F::kQuant)
-          x *= kp[key];
-        s[c][r] = x * col_scale[c];
-      }
-    }
-    uint32_t seen[NC];  // bit r: this row sees the key of register r
+    uint32_t seen[NC];  // bit 4 u + r: this row sees the key
 #pragma unroll
     for (int c = 0; c < NC; ++c) seen[c] = 0xFFFFu;
     if (look) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const uint64_t* words = p.mask ? p.mask + (size_t)b * p.mask_stride + (size_t)t_of[c] * p.mask_words : nullptr;
-        for (int r = 0; r < 16; ++r) {
+        for (int i = 0; i < 4 * U; ++i) {
           int pos;
-          bool see = slots.position(k0 + acc_key(r, half), pos) && t_of[c] < n;
+          bool see = slots.position(k0 + step_key(g, i), pos) && t_of[c] < n;
           const int draft = pos - first_new;
           if (see && draft >= 0) see = words ? (words[draft >> 6] >> (draft & 63)) & 1 : draft <= t_of[c];
-          if (!see) seen[c] &= ~(1u << r);
+          if (!see) seen[c] &= ~(1u << i);
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!((seen[c] >> r) & 1)) s[c][r] = kMasked;
       }
     }
 
-    // ---- running maximum; the sums so far are brought to it
+    // ---- probabilities, times V's scale
+    f32x4 v_scale[U], v_low[U];
+    if constexpr (F::kQuant) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v_scale[u] = *(const f32x4*)(vp + 16 * u + 4 * g);
+        if constexpr (FORMAT == KVCRUSH_I4) v_low[u] = *(const f32x4*)(vp + 2 * kTile + 16 * u + 4 * g);
+      }
+    }
+    f32x4 w[NC][U];
+    auto weigh = [&](int c, f32x4 (&pr)[U]) {  // pr: probabilities, w: times scales
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][u][r], col_scale[c], -m[c]));
+          if constexpr (F::kQuant)
+            w[c][u][r] = pr[u][r] * v_scale[u][r];
+          else
+            w[c][u][r] = pr[u][r];
+        }
+      if (look) {  // (a logit or a scale that the row does not see may be anything)
+#pragma unroll
+        for (int i = 0; i < 4 * U; ++i)
+          if (!((seen[c] >> i) & 1)) pr[i / 4][i % 4] = w[c][i / 4][i % 4] = 0.0f;
+      }
+    };
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      float t = s[c][0];
+      f32x4 pr[U];
+      weigh(c, pr);
+      float wide = w[c][0][0], top = pr[0][0];
 #pragma unroll
-      for (int r = 1; r < 16; ++r) t = fmaxf(t, s[c][r]);
-      t = fmaxf(t, __shfl_xor(t, 32));
-      const float mn = fmaxf(m[c], t), a = __builtin_amdgcn_exp2f(m[c] - mn);
-      m[c] = mn;
-      l[c] *= a;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[c][r] = __builtin_amdgcn_exp2f(s[c][r] - mn);
-        l[c] += s[c][r];
+      for (int i = 1; i < 4 * U; ++i) {
+        wide = fmaxf(wide, w[c][i / 4][i % 4]);
+        if constexpr (F::kQuant) top = fmaxf(top, pr[i / 4][i % 4]);
       }
-      float down = a;
-      if constexpr (F::kQuant) {
-        // what multiplies the codes: probability x scale, as a share of the largest such product of this row so far
-        if constexpr (FORMAT == KVCRUSH_I4) z[c] *= a;
-        float top = 0.0f;
+      if (__ballot(wide > 0x1p8f || (F::kQuant && top > 0x1p96f)) != 0) {
+        float most = kNegBig;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = acc_key(r, half);
-          const bool see = (seen[c] >> r) & 1;
-          if constexpr (FORMAT == KVCRUSH_I4) z[c] = see ? __builtin_fmaf(s[c][r], vp[kTile + key], z[c]) : z[c];
-          s[c][r] = see ? s[c][r] * vp[key] : 0.0f;
-          top = fmaxf(top, s[c][r]);  // (a NaN is passed over)
+        for (int i = 0; i < 4 * U; ++i) {
+          float x = s[c][i / 4][i % 4] * col_scale[c];
+          if constexpr (F::kQuant) x = fmaxf(x + __builtin_amdgcn_logf(v_scale[i / 4][i % 4]), x - 96.0f);
+          if (!look || ((seen[c] >> i) & 1)) most = fmaxf(most, x);
         }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float before = unit[c] * a;
-        unit[c] = fmaxf(before, top);
-        const float inv = unit[c] > 0.0f ? 1.0f / unit[c] : 0.0f;
-        down = before * inv;
+        const float mn = fmaxf(m[c], row_max(most)), a = __builtin_amdgcn_exp2f(m[c] - mn);
+        m[c] = mn;
+        l[c] *= a;
+        if constexpr (FORMAT == KVCRUSH_I4) z[c] *= a;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[c][r] *= inv;
+        for (int d = 0; d < F::kDTiles; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[c][d][r] *= a;
+        weigh(c, pr);
       }
 #pragma unroll
-      for (int d = 0; d < F::kDTiles; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[c][d][r] *= down;
+      for (int i = 0; i < 4 * U; ++i) {
+        l[c] += pr[i / 4][i % 4];
+        if constexpr (FORMAT == KVCRUSH_I4) {
+          if (!look || ((seen[c] >> i) & 1)) z[c] = __builtin_fmaf(pr[i / 4][i % 4], v_low[i / 4][i % 4], z[c]);
+        }
+      }
     }
     if constexpr (FORMAT != KVCRUSH_I8 && FORMAT != KVCRUSH_I4) {
       if (look) {
@@ -438,40 +562,34 @@ __global__ __launch_bounds__(F::kWaves * KVC_WAVE) void attend_kernel(AttendPara
         uint32_t bad = 0;
 #pragma unroll
         for (int j = 0; j < F::kLoads; ++j) {
-          const u32x4 w = *(const u32x4*)(vt + j * 1024 + lane * 16);
+          const u32x4 x = *(const u32x4*)(vt + j * 1024 + lane * 16);
           bool odd = false;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) odd = odd || !all_finite<FORMAT>(w[i]);
-          int row, chunk;
-          F::template chunk_of<true>(j * 64 + lane, row, chunk);
-          if (odd) bad |= 1u << row;
+          for (int i = 0; i < 4; ++i) odd = odd || !all_finite<FORMAT>(x[i]);
+          if (odd) bad |= 1u << (in_tile[j] / F::kRow);
         }
         bad = kvc::wave_reduce(bad, 0u, [](uint32_t x, uint32_t y) { return x | y; });
         if (bad) {
           for (uint32_t left = bad; left; left &= left - 1) {
-            const int key = __builtin_ctz(left), reg = (key & 3) + 4 * (key >> 3), from = col + 32 * ((key >> 2) & 1);
+            const int key = __builtin_ctz(left), reg = 4 * (key >> 4) + (key & 3), from = col + 16 * ((key >> 2) & 3);
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
               float x = 0.0f;
 #pragma unroll
-              for (int r = 0; r < 16; ++r) x = r == reg ? s[c][r] : x;
+              for (int i = 0; i < 4 * U; ++i) x = i == reg ? w[c][i / 4][i % 4] : x;
               x = __shfl(x, from);
               if (__shfl((int)((seen[c] >> reg) & 1), from)) {
 #pragma unroll
                 for (int d = 0; d < F::kDTiles; ++d)
 #pragma unroll
-                  for (int r = 0; r < 16; ++r)
-                    o[c][d][r] += x * tile_value<F>(vt, key, d * 32 + acc_key(r, half));
+                  for (int r = 0; r < 4; ++r) o[c][d][r] += x * tile_value<F>(vt, key, d * 16 + 4 * g + r);
               }
             }
           }
           kvc::wave_fence();
 #pragma unroll
-          for (int j = 0; j < F::kLoads; ++j) {
-            int row, chunk;
-            F::template chunk_of<true>(j * 64 + lane, row, chunk);
-            if ((bad >> row) & 1) *(u32x4*)(stage + F::kTileBytes + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-          }
+          for (int j = 0; j < F::kLoads; ++j)
+            if ((bad >> (in_tile[j] / F::kRow)) & 1) *(u32x4*)(const_cast<char*>(vt) + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
           kvc::wave_fence();
         }
       }
@@ -480,193 +598,158 @@ __global__ __launch_bounds__(F::kWaves * KVC_WAVE) void attend_kernel(AttendPara
     // ---- values
     if constexpr (F::kBits == 32) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+      for (int r = 0; r < 4; ++r) {
 #pragma unroll
         for (int d = 0; d < F::kDTiles; ++d) {
-          const int e = d * 32 + col;  // value
-          const float v = *(const float*)(vt + F::template chunk_at<true>(acc_key(r, half), e >> 2) + (e & 3) * 4);
+          const int e = d * 16 + col;  // value
+          const float v = *(const float*)(vt + F::chunk_at(4 * g + r, e >> 2) + (e & 3) * 4);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[c][r], o[c][d], 0, 0, 0);
+          for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, w[c][0][r], o[c][d], 0, 0, 0);
         }
       }
     } else {
-      // a probability is the sum of two 16-bit values: its rounding and what that left
+      // A weight is the sum of two 16-bit values, its rounding and what that left: rounded once, it would cost the result
+      // about as much again as its own rounding (measured: 1.4 times the error).
       constexpr int P = FORMAT == KVCRUSH_BF16 ? KVCRUSH_BF16 : KVCRUSH_F16;
-      u32x4 hi[NC][2], lo[NC][2];
+      u32x4 hi[NC][U / 2], lo[NC][U / 2];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = s[c][8 * st + 2 * i], y = s[c][8 * st + 2 * i + 1];
-            // (values from here on: otherwise the compiler may round the product behind x to 16 bits in one step for
-            // `hi` and in two for what `hi` left)
-            asm("" : "+v"(x), "+v"(y));
-            const uint32_t w = pack2<P>(x, y);
-            float xh, yh;
-            if constexpr (P == KVCRUSH_BF16) {
-              xh = __uint_as_float(w << 16);
-              yh = __uint_as_float(w & 0xFFFF0000u);
-            } else {
-              const f16x2 f = as_f16x2(w);
-              xh = (float)f[0];
-              yh = (float)f[1];
-            }
-            hi[c][st][i] = w;
-            lo[c][st][i] = pack2<P>(x - xh, y - yh);
+        for (int i = 0; i < 2 * U; ++i) {
+          float x = w[c][i / 2][2 * (i % 2)], y = w[c][i / 2][2 * (i % 2) + 1];
+          // (values from here on: otherwise the compiler may round the product behind x to 16 bits in one step for
+          // `hi` and in two for what `hi` left)
+          asm("" : "+v"(x), "+v"(y));
+          const uint32_t both = pack2<P>(x, y);
+          float xh, yh;
+          if constexpr (P == KVCRUSH_BF16) {
+            xh = __uint_as_float(both << 16);
+            yh = __uint_as_float(both & 0xFFFF0000u);
+          } else {
+            const f16x2 f = as_f16x2(both);
+            xh = (float)f[0];
+            yh = (float)f[1];
           }
+          hi[c][i / 4][i % 4] = both;
+          lo[c][i / 4][i % 4] = pack2<P>(x - xh, y - yh);
+        }
 #pragma unroll
       for (int d = 0; d < F::kDTiles; ++d) {
         u32x2 codes;
         if constexpr (F::kBits == 4) codes = v_codes4<F>(vt, lane, d);
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
+        for (int ks = 0; ks < U / 2; ++ks) {
           u32x4 vf;
           if constexpr (F::kBits == 4)
-            vf = codes8_to_f16(codes[st]);
+            vf = codes8_to_f16(codes[ks]);
           else
-            vf = v_frag<F>(vt, lane, d, st);
+            vf = v_frag<F>(vt, lane, d, ks);
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            mma16<FORMAT>(o[c][d], vf, hi[c][st]);
-            mma16<FORMAT>(o[c][d], vf, lo[c][st]);
+            mma<FORMAT>(o[c][d], vf, hi[c][ks]);
+            mma<FORMAT>(o[c][d], vf, lo[c][ks]);
           }
         }
       }
     }
-    kvc::wave_fence();  // the stage's last reads come before its next copies
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 
-  // ---- the waves' rows are brought to one maximum and added up
-  float* ml = (float*)lds_all;                                     // [waves][NC][32][2]
-  float* sums = (float*)(lds_all + F::kWaves * NC * 256);          // [waves / 2][64 lanes][16 D / 32 + 1]
+  // ---- the waves' rows are brought to one reference and added up
+  constexpr int kPitch = D + 4;
+  float2* ml = (float2*)lds_all;                                    // [waves][NC][16]
+  float* sums = (float*)(lds_all + kWaves * NC * 128);           // [waves][16][kPitch]
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    l[c] += __shfl_xor(l[c], 32);
-    if (t_of[c] >= n) {  // padding: it sees nothing
-      l[c] = 0.0f;
-      m[c] = kNegBig;
-    }
-    if constexpr (FORMAT == KVCRUSH_I4) z[c] += __shfl_xor(z[c], 32);
-    if constexpr (F::kQuant) {
+    l[c] = row_sum(l[c]);
+    if constexpr (FORMAT == KVCRUSH_I4) {
+      z[c] = row_sum(z[c]);
 #pragma unroll
       for (int d = 0; d < F::kDTiles; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if constexpr (FORMAT == KVCRUSH_I4)
-            o[c][d][r] = __builtin_fmaf(o[c][d][r], unit[c], z[c]);
-          else
-            o[c][d][r] *= unit[c];
-        }
+        for (int r = 0; r < 4; ++r) o[c][d][r] += z[c];
+    }
+    if (t_of[c] >= n) {  // padding: it sees nothing
+      l[c] = 0.0f;
+      m[c] = kNegBig;
     }
   }
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-    if (half == 0) *(float2*)(ml + ((wave * NC + c) * 32 + col) * 2) = make_float2(m[c], l[c]);
+    if (g == 0) ml[(wave * NC + c) * 16 + col] = make_float2(m[c], l[c]);
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    float mt = kNegBig, lt = 0.0f;
+    float top = kNegBig;
 #pragma unroll
-    for (int w = 0; w < F::kWaves; ++w) mt = fmaxf(mt, ml[((w * NC + c) * 32 + col) * 2]);
-#pragma unroll
-    for (int w = 0; w < F::kWaves; ++w) {
-      const float2 x = *(const float2*)(ml + ((w * NC + c) * 32 + col) * 2);
-      lt += x.y * __builtin_amdgcn_exp2f(x.x - mt);
-    }
-    const float a = __builtin_amdgcn_exp2f(m[c] - mt);
-    l[c] = lt;
-    m[c] = mt;
-    constexpr int kPer = 16 * F::kDTiles;
+    for (int x = 0; x < kWaves; ++x) top = fmaxf(top, ml[(x * NC + c) * 16 + col].x);
+    const float a = __builtin_amdgcn_exp2f(m[c] - top);
+    if (c > 0) __syncthreads();
 #pragma unroll
     for (int d = 0; d < F::kDTiles; ++d)
+      *(f32x4*)(sums + (wave * 16 + col) * kPitch + d * 16 + 4 * g) = f32x4{o[c][d][0] * a, o[c][d][1] * a, o[c][d][2] * a, o[c][d][3] * a};
+    __syncthreads();
+    // four values a thread
+    for (int i = tid; i < 16 * (D / 4); i += kWaves * KVC_WAVE) {
+      const int row = i / (D / 4), e = i % (D / 4) * 4, r = row0 + c * 16 + row;
+      if (r >= rows) break;  // (rows ascend with i)
+      const int t = p.blocks ? t_list : r / p.G, head = h * p.G + (p.blocks ? r : r - t * p.G);
+      float most = kNegBig, total = 0.0f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[c][d][r] *= a;
-    for (int left = F::kWaves / 2; left > 0; left /= 2) {  // waves left .. 2 left - 1 hand theirs to 0 .. left - 1
-      __syncthreads();
-      if (wave >= left && wave < 2 * left) {
+      for (int x = 0; x < kWaves; ++x) most = fmaxf(most, ml[(x * NC + c) * 16 + row].x);
+      f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sums[((wave - left) * kPer + i) * 64 + lane] = o[c][i / 16][i % 16];
+      for (int x = 0; x < kWaves; ++x) {
+        const float2 y = ml[(x * NC + c) * 16 + row];
+        total += y.y * __builtin_amdgcn_exp2f(y.x - most);
+        sum += *(const f32x4*)(sums + (x * 16 + row) * kPitch + e);
       }
-      __syncthreads();
-      if (wave < left) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) o[c][i / 16][i % 16] += sums[(wave * kPer + i) * 64 + lane];
+      const size_t at = ((size_t)b * p.Hq + head) * p.T + t;
+      if (p.n_split > 1) {
+        if (e == 0) p.part_ml[at * p.n_split + split] = make_float2(most, total);
+        *(f32x4*)(p.part_o + (at * p.n_split + split) * D + e) = sum;
+      } else {
+        store_result(p, b, head, t, e, most, total, sum);
       }
-    }
-  }
-  if (wave != 0) return;
-#pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    if (!live[c]) continue;
-    const int r = row0 + c * 32 + col, t = t_of[c], g = p.blocks ? r : r - t * p.G;
-    if (p.n_split > 1) {
-      const size_t at = (((size_t)bh * p.G + g) * p.T + t) * p.n_split + split;
-      if (half == 0) p.part_ml[at] = make_float2(m[c], l[c]);
-#pragma unroll
-      for (int d = 0; d < F::kDTiles; ++d)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *(float4*)(p.part_o + at * D + d * 32 + 8 * q + 4 * half) =
-              make_float4(o[c][d][4 * q], o[c][d][4 * q + 1], o[c][d][4 * q + 2], o[c][d][4 * q + 3]);
-    } else {
-      const float inv = l[c] > 0.0f || l[c] != l[c] ? 1.0f / l[c] : 0.0f;
-      const int head = h * p.G + g;
-      if (p.lse && half == 0)
-        p.lse[((size_t)b * p.Hq + head) * p.T + t] = l[c] == 0.0f ? -__builtin_inff() : (m[c] + __builtin_amdgcn_logf(l[c])) * kLn2;
-      const size_t at = (size_t)b * p.out_stride[0] + (size_t)head * p.out_stride[1] + (size_t)t * p.out_stride[2];
-#pragma unroll
-      for (int d = 0; d < F::kDTiles; ++d)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const size_t e = at + d * 32 + 8 * q + 4 * half;
-          float x[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = l[c] == 0.0f ? 0.0f : o[c][d][4 * q + i] * inv;
-          if (FORMAT == KVCRUSH_F32)
-            *(float4*)(p.out + e * 4) = make_float4(x[0], x[1], x[2], x[3]);
-          else if (p.q_dtype == KVCRUSH_BF16)
-            *(u32x2*)(p.out + e * 2) = u32x2{pack2<KVCRUSH_BF16>(x[0], x[1]), pack2<KVCRUSH_BF16>(x[2], x[3])};
-          else
-            *(u32x2*)(p.out + e * 2) = u32x2{pack2<KVCRUSH_F16>(x[0], x[1]), pack2<KVCRUSH_F16>(x[2], x[3])};
-        }
     }
   }
 }
 
-// The pieces of a row (query t of head hq): D / 4 lanes, four values each.
+// The pieces of a row (query t of a head): D / 4 lanes of four values, the pieces dealt to the 256 / (D / 4) such groups of
+// the workgroup.
 template <int D>
 __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
-  constexpr int kLanes = D / 4;
-  const long long row = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;  // (b * Hq + head) * T + t
-  if (row >= (long long)p.c.B * p.Hq * p.T) return;
-  const int e = threadIdx.x % kLanes * 4;
-  const float2* ml = p.part_ml + row * p.n_split;
-  float m = kNegBig;
-  for (int i = 0; i < p.n_split; ++i) m = fmaxf(m, ml[i].x);
-  float l = 0.0f;
-  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int i = 0; i < p.n_split; ++i) {
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+  __shared__ f32x4 sums[kGroups][kLanes];
+  __shared__ float2 mls[kGroups];
+  const int row = blockIdx.x, part = threadIdx.x / kLanes, e = threadIdx.x % kLanes * 4;  // row = (b * Hq + head) * T + t
+  const float2* ml = p.part_ml + (size_t)row * p.n_split;
+  const float* o = p.part_o + (size_t)row * p.n_split * D + e;
+  float m = kNegBig, total = 0.0f;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = part; i < p.n_split; i += kGroups) {
     const float2 x = ml[i];
-    const float a = __builtin_amdgcn_exp2f(x.x - m);
-    const float4 y = *(const float4*)(p.part_o + (row * p.n_split + i) * D + e);
-    l += x.y * a;
-    o.x += y.x * a, o.y += y.y * a, o.z += y.z * a, o.w += y.w * a;
+    const f32x4 y = *(const f32x4*)(o + (size_t)i * D);
+    const float mn = fmaxf(m, x.x), a = __builtin_amdgcn_exp2f(m - mn), c = __builtin_amdgcn_exp2f(x.x - mn);
+    m = mn;
+    total = total * a + x.y * c;
+    sum = sum * a + y * c;
   }
-  const int t = (int)(row % p.T), head = (int)(row / p.T % p.Hq), b = (int)(row / p.T / p.Hq);
-  if (p.lse && e == 0) p.lse[row] = l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (l == 0.0f) o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  const size_t at = (size_t)b * p.out_stride[0] + (size_t)head * p.out_stride[1] + (size_t)t * p.out_stride[2] + e;
-  if (p.q_dtype == KVCRUSH_F32)
-    *(float4*)(p.out + at * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  else if (p.q_dtype == KVCRUSH_BF16)
-    *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_BF16>(o.x * inv, o.y * inv), pack2<KVCRUSH_BF16>(o.z * inv, o.w * inv)};
-  else
-    *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_F16>(o.x * inv, o.y * inv), pack2<KVCRUSH_F16>(o.z * inv, o.w * inv)};
+  sums[part][e / 4] = sum;
+  if (e == 0) mls[part] = make_float2(m, total);
+  __syncthreads();
+  if (part != 0) return;
+#pragma unroll
+  for (int i = 1; i < kGroups; ++i) {
+    const float2 x = mls[i];
+    const f32x4 y = sums[i][e / 4];
+    const float mn = fmaxf(m, x.x), a = __builtin_amdgcn_exp2f(m - mn), c = __builtin_amdgcn_exp2f(x.x - mn);
+    m = mn;
+    total = total * a + x.y * c;
+    sum = sum * a + y * c;
+  }
+  store_result(p, row / p.T / p.Hq, row / p.T % p.Hq, row % p.T, e, m, total, sum);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -685,20 +768,17 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   if (!(a->softmax_scale >= 0.0f) || a->softmax_scale > 1.0e6f) return KVCRUSH_ERR_INVALID_ARG;
   if (a->mask_stride < 0) return KVCRUSH_ERR_INVALID_ARG;
   if (a->blocks && (a->n_list < 1 || a->unit < 1)) return KVCRUSH_ERR_INVALID_ARG;
-  if (a->T > 1024 || (long long)c->B * c->Hkv > 65535 || c->capacity > (1 << 30)) return KVCRUSH_ERR_UNSUPPORTED;
+  if (a->T > 1024 || (long long)c->B * a->Hq * a->T > (1 << 24) || (long long)c->B * c->Hkv > 65535 || c->capacity > (1 << 30)) return KVCRUSH_ERR_UNSUPPORTED;
   if (a->blocks && (long long)a->n_list * a->unit >= (1 << 30)) return KVCRUSH_ERR_UNSUPPORTED;
   plan.G = a->Hq / c->Hkv;
   plan.rows = (long long)c->B * a->Hq * a->T;
   const long long r = a->blocks ? plan.G : (long long)plan.G * a->T;
-  plan.NC = r > 32 ? 2 : 1;
-  const long long tiles = (r + 32 * plan.NC - 1) / (32 * plan.NC);
-  if (tiles > 1 && a->blocks) plan.NC = 2;
-  const long long y = a->blocks ? a->T : tiles;
-  if (y > 65535 || (a->blocks && tiles > 1)) return KVCRUSH_ERR_UNSUPPORTED;
-  plan.row_tiles = (int)y;
+  plan.NC = r > 32 ? 4 : r > 16 ? 2 : 1;
+  const long long tiles = (r + 16 * plan.NC - 1) / (16 * plan.NC) * (a->blocks ? a->T : 1);
+  plan.row_tiles = (int)tiles;
   const long long keys = a->blocks ? std::min<long long>((long long)a->n_list * a->unit, c->capacity) : c->S;
-  const long long base = (long long)c->B * c->Hkv * y;
-  long long split = (512 + base - 1) / base;
+  const long long base = (long long)c->B * c->Hkv * tiles;
+  long long split = (256 + base - 1) / base;
   split = std::min(split, (keys + 255) / 256);
   plan.n_split = (int)std::max(1ll, std::min<long long>(split, kMaxSplit));
   return KVCRUSH_OK;
@@ -710,14 +790,21 @@ size_t plan_bytes(const Plan& p, int D) {
 }
 
 template <class F, int NC>
-kvcrush_status launch_attend(const AttendParams& p, int row_tiles, hipStream_t stream) {
-  constexpr int kLoop = F::kWaves * (F::kStage + kAhead * 4);
-  constexpr int kEnd = F::kWaves * NC * 256 + F::kWaves / 2 * F::kDTiles * 16 * 256;
+kvcrush_status launch_attend(const AttendParams& p, hipStream_t stream) {
+  constexpr int kWaves = F::waves(NC);
+  constexpr int kLoop = kWaves * (F::kStages * F::kStage + kAhead * 4);
+  constexpr int kEnd = kWaves * (NC * 128 + 16 * (F::D + 4) * 4);
   constexpr int kLds = kLoop > kEnd ? kLoop : kEnd;
   static_assert(kLds <= kvc::kLdsPerWorkgroup, "LDS of a workgroup");
   kvcrush_status st = kvc::allow_large_lds<attend_kernel<F, NC>>(0);
   if (st != KVCRUSH_OK) return st;
-  return kvc::launch(attend_kernel<F, NC>, dim3(p.n_split, row_tiles, p.c.B * p.c.Hkv), dim3(F::kWaves * KVC_WAVE), kLds, stream, p);
+  const dim3 grid((unsigned)((p.groups + 7) / 8 * 8) * p.row_tiles);
+  return kvc::launch(attend_kernel<F, NC>, grid, dim3(kWaves * KVC_WAVE), kLds, stream, p);
+}
+
+template <class F>
+kvcrush_status launch_rows(const AttendParams& p, int NC, hipStream_t stream) {
+  return NC == 4 ? launch_attend<F, 4>(p, stream) : NC == 2 ? launch_attend<F, 2>(p, stream) : launch_attend<F, 1>(p, stream);
 }
 
 }  // namespace
@@ -758,21 +845,18 @@ extern "C" kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcru
   p.G = plan.G;
   p.T = args->T;
   p.n_split = plan.n_split;
+  p.row_tiles = plan.row_tiles;
+  p.groups = cache->B * cache->Hkv * plan.n_split;
   p.q_dtype = args->dtype;
   p.scale_log2 = (float)(1.4426950408889634 *
                          (args->softmax_scale != 0.0f ? (double)args->softmax_scale : 1.0 / sqrt((double)D)));
   hipStream_t stream = (hipStream_t)hip_stream;
   st = with_format(cache->format, [&](auto fmt) -> kvcrush_status {
     constexpr int FMT = decltype(fmt)::value;
-    if (D == 128)
-      return plan.NC == 2 ? launch_attend<Fmt<FMT, 128>, 2>(p, plan.row_tiles, stream)
-                          : launch_attend<Fmt<FMT, 128>, 1>(p, plan.row_tiles, stream);
-    return plan.NC == 2 ? launch_attend<Fmt<FMT, 64>, 2>(p, plan.row_tiles, stream)
-                        : launch_attend<Fmt<FMT, 64>, 1>(p, plan.row_tiles, stream);
+    return D == 128 ? launch_rows<Fmt<FMT, 128>>(p, plan.NC, stream) : launch_rows<Fmt<FMT, 64>>(p, plan.NC, stream);
   });
   if (st != KVCRUSH_OK || plan.n_split == 1) return st;
-  const int per = 256 / (D / 4);
-  const dim3 grid((unsigned)((plan.rows + per - 1) / per));
+  const dim3 grid((unsigned)plan.rows);
   return D == 128 ? kvc::launch(attend_merge_kernel<128>, grid, dim3(256), 0, stream, p)
                   : kvc::launch(attend_merge_kernel<64>, grid, dim3(256), 0, stream, p);
 }
