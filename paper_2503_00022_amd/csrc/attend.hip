@@ -64,9 +64,10 @@ struct Fmt {
   static constexpr int kStage = 2 * kTileBytes + kParamLoads * 256;
   static constexpr int kStages = 2;
   // Eight waves where LDS and registers have room for them: two to a SIMD, so that one's matrix instructions run beside
-  // the other's arithmetic.
-  static constexpr int waves(int NC) {
-    return NC == 4 || (NC == 2 && kBits == 4) || kStage * kStages * 8 + 8 * kAhead * 4 > kvc::kLdsPerWorkgroup ? 4 : 8;
+  // the other's arithmetic.  RW of them share a tile.
+  static constexpr int lds(int waves, int RW) { return waves / RW * kStages * kStage + waves * kAhead * 4; }
+  static constexpr int waves(int NC, int RW) {
+    return (NC == 2 && kBits == 4) || lds(8, RW) > kvc::kLdsPerWorkgroup ? 4 : 8;
   }
   static constexpr int kSteps = D / 32;            // matrix steps of 32 values along D (16-bit operands)
   static constexpr int kDTiles = D / 16;
@@ -208,19 +209,17 @@ __device__ __forceinline__ float tile_value(const char* tile, int key, int d) {
   return (float)as_f16x2(h[0])[0];
 }
 
-// Position of a key slot, and whether there is a token.
+// Position of a key slot, and whether there is a token (without branches, so that many are looked up at a time).
 struct Slots {
   const int32_t* list;  // this query's blocks, or null
   int n, unit, L;
   __device__ bool position(int slot, int& pos) const {
     pos = slot;
-    if (slot >= n) return false;
-    if (list) {
-      const int e = slot / unit, blk = list[e];
-      if (blk < 0 || (e > 0 && blk <= list[e - 1]) || blk > (L - 1) / unit) return false;
-      pos = blk * unit + (slot - e * unit);
-    }
-    return pos < L;
+    if (!list) return slot < n;
+    const int e = min(slot, n - 1) / unit, blk = list[e], before = list[max(e - 1, 0)];
+    const bool there = (slot < n) & (blk >= 0) & ((e == 0) | (blk > before)) & (blk <= (L - 1) / unit);
+    pos = (there ? blk : 0) * unit + (slot - e * unit);
+    return there & (pos < L);
   }
 };
 
@@ -262,13 +261,16 @@ __device__ __forceinline__ void store_result(const AttendParams& p, int b, int h
     *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_F16>(x[0], x[1]), pack2<KVCRUSH_F16>(x[2], x[3])};
 }
 
-template <class F, int NC>
-__global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendParams p) {
-  constexpr int kWaves = F::waves(NC);
+// RW: waves that share a tile, each with 16 NC rows of its own.  One: the waves are on their own, and nobody waits for
+// another's copies.  More: they copy a share each and meet at a barrier per tile, so that many rows cost one reading of
+// the keys.
+template <class F, int NC, int RW>
+__global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(AttendParams p) {
+  constexpr int kWaves = F::waves(NC, RW), kGroups = kWaves / RW;
   constexpr int D = F::D, FORMAT = F::FORMAT, kTile = F::kTile, U = F::kSub;
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   const int tid = threadIdx.x, lane = kvc::lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / KVC_WAVE);
-  const int g = lane >> 4, col = lane & 15;
+  const int g = lane >> 4, col = lane & 15, key_group = wave / RW, row_wave = wave % RW;
   // Workgroups with numbers 8 apart run on one chiplet, one after the other: the row tiles of a piece, which read the same
   // keys, are put there side by side.
   const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, row_tile = place % p.row_tiles;
@@ -277,9 +279,10 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
   const int bh = group / p.n_split, split = group - bh * p.n_split, b = bh / p.c.Hkv, h = bh - b * p.c.Hkv;
   const int L = p.c.length(b), n = new_tokens(p.n_new, b, p.T, L);
   // with lists, a query's G heads are the rows
-  const int tiles_of_query = (p.G + 16 * NC - 1) / (16 * NC);
+  constexpr int kRows = 16 * NC * RW;
+  const int tiles_of_query = (p.G + kRows - 1) / kRows;
   const int t_list = p.blocks ? row_tile / tiles_of_query : 0;
-  const int row0 = (p.blocks ? row_tile % tiles_of_query : row_tile) * 16 * NC;
+  const int row0 = (p.blocks ? row_tile % tiles_of_query : row_tile) * kRows;
   const int rows = p.blocks ? p.G : p.G * p.T;
 
   Slots slots;
@@ -288,65 +291,90 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
   slots.n = p.blocks ? (t_list < n ? p.n_list * p.unit : 0) : n > 0 ? L : 0;
   slots.L = L;
 
-  // this wave's tiles: a contiguous piece of the workgroup's
+  // this wave's (or its group's) tiles: a contiguous piece of the workgroup's
   const int tiles = (slots.n + kTile - 1) / kTile, per_wg = (tiles + p.n_split - 1) / p.n_split;
   const int wg0 = min(split * per_wg, tiles), wg1 = min(wg0 + per_wg, tiles);
-  const int per_wave = (wg1 - wg0 + kWaves - 1) / kWaves;
-  const int tile0 = min(wg0 + wave * per_wave, wg1), tile1 = min(tile0 + per_wave, wg1);
+  const int per_group = (wg1 - wg0 + kGroups - 1) / kGroups;
+  const int tile0 = min(wg0 + key_group * per_group, wg1), tile1 = min(tile0 + per_group, wg1);
 
-  // ---- copies of tiles into this wave's stages
-  char* own = lds_all + wave * (F::kStages * F::kStage + kAhead * 4);
+  // ---- copies of tiles into this group's stages
+  char* own = lds_all + key_group * (F::kStages * F::kStage);
   const uint32_t own_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)own);
-  int* places = (int*)(own + F::kStages * F::kStage);  // token of each slot; bit 31: the slot has to be looked at
+  // token of each slot (a table of each wave's own); bit 31: the slot has to be looked at
+  int* places = (int*)(lds_all + kGroups * F::kStages * F::kStage) + wave * kAhead;
   const size_t row_base = p.c.base(b, h), row_step = p.c.step();
   const bool lookup = p.c.table || p.blocks;
   const int first_new = L - n;
   uint32_t looks = 0;  // bit i % 32: tile tile0 + i has such slots (lookups only)
-  uint32_t in_tile[F::kLoads];  // this lane's bytes of a tile whose rows lie one behind the other
+  // A tile is 2 kLoads pieces of 1 KiB, K's and behind them V's; wave row_wave of a group copies pieces row_wave,
+  // row_wave + RW, ..  in_tile: this lane's bytes of a piece, in a tile whose rows lie one behind the other.
+  constexpr int kOwn = 2 * F::kLoads / RW;
+  static_assert(2 * F::kLoads % RW == 0, "the waves of a group copy alike");
+  uint32_t in_tile[kOwn];
 #pragma unroll
-  for (int j = 0; j < F::kLoads; ++j) {
+  for (int j = 0; j < kOwn; ++j) {
     int row, chunk;
-    F::chunk_of(j * 64 + lane, row, chunk);
+    F::chunk_of((j * RW + row_wave) % F::kLoads * 64 + lane, row, chunk);
     in_tile[j] = row * F::kRow + chunk * 16;
   }
-  constexpr int kCopies = 2 * F::kLoads + F::kParamLoads;
+  constexpr int kCopies = kOwn + F::kParamLoads;
   auto issue = [&](int tile) {
     const int k0 = tile * kTile, i = tile - tile0, ahead = (i * kTile) & (kAhead - 1);
-    const uint32_t dst = own_at + (i % F::kStages) * F::kStage;
+    const uint32_t stage = own_at + (i % F::kStages) * F::kStage, dst = stage + row_wave * 1024;
     if (lookup && ahead == 0) {
-      const int end = min(kAhead, (tile1 - tile) * kTile);
-      for (int x = lane; x < end; x += KVC_WAVE) {
-        int pos;
-        const bool there = slots.position(k0 + x, pos);
-        places[x] = p.c.token(b, there ? pos : 0) | (!there || pos >= first_new ? (int)0x80000000 : 0);
+      // (branches only around the loops, so that a loop's loads are all on their way before the first is used)
+      constexpr int kEach = kAhead / KVC_WAVE;
+      int at[kEach];
+      uint32_t marked = 0;
+#pragma unroll
+      for (int x = 0; x < kEach; ++x) at[x] = k0 + x * KVC_WAVE + lane;
+      if (slots.list) {
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) {
+          int pos;
+          const bool there = slots.position(at[x], pos);
+          if (!there || pos >= first_new) marked |= 1u << x;
+          at[x] = there ? pos : 0;
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) {
+          if (at[x] >= first_new) marked |= 1u << x;
+          at[x] = at[x] < L ? at[x] : 0;
+        }
       }
+      if (p.c.table) {
+#pragma unroll
+        for (int x = 0; x < kEach; ++x) at[x] = p.c.paged_token(b, at[x]);
+      }
+#pragma unroll
+      for (int x = 0; x < kEach; ++x)
+        places[x * KVC_WAVE + lane] = at[x] | ((marked >> x) & 1 ? (int)0x80000000 : 0);
       kvc::wave_fence();
     }
     if (!lookup && k0 + kTile <= L) {
       const size_t from = (row_base + k0) * F::kRow;
       const char *k = kvc::tiles::wave_uniform(p.c.k + from), *v = kvc::tiles::wave_uniform(p.c.v + from);
 #pragma unroll
-      for (int j = 0; j < F::kLoads; ++j) copy16(k, in_tile[j], dst + j * 1024);
-#pragma unroll
-      for (int j = 0; j < F::kLoads; ++j) copy16(v, in_tile[j], dst + F::kTileBytes + j * 1024);
+      for (int j = 0; j < kOwn; ++j) copy16(j * RW + row_wave < F::kLoads ? k : v, in_tile[j], dst + j * RW * 1024);
     } else {
 #pragma unroll
-      for (int j = 0; j < F::kLoads; ++j) {
+      for (int j = 0; j < kOwn; ++j) {
         const int row = in_tile[j] / F::kRow;
         const int tok = lookup ? places[ahead + row] & 0x7FFFFFFF : min(k0 + row, L - 1);
         const size_t from = (row_base + (size_t)tok * row_step) * F::kRow + in_tile[j] % F::kRow;
-        copy16(p.c.k + from, dst + j * 1024);
-        copy16(p.c.v + from, dst + F::kTileBytes + j * 1024);
+        copy16((j * RW + row_wave < F::kLoads ? p.c.k : p.c.v) + from, dst + j * RW * 1024);
       }
     }
     if constexpr (F::kQuant) {
+      // (all of them by every wave of a group: the same bytes to the same place, and equal numbers of copies to wait for)
 #pragma unroll
       for (int j = 0; j < F::kParamLoads; ++j) {
         // [parameter][K, V][key] floats
         const int e = j * 64 + lane, key = e % kTile, which = (e / kTile) & 1, par = e / (2 * kTile);
         const int tok = lookup ? places[ahead + key] & 0x7FFFFFFF : min(k0 + key, L - 1);
         const float* src = which ? p.c.v_param : p.c.k_param;
-        copy4((const char*)(src + (row_base + (size_t)tok * row_step) * F::kParam + par), dst + 2 * F::kTileBytes + j * 256);
+        copy4((const char*)(src + (row_base + (size_t)tok * row_step) * F::kParam + par), stage + 2 * F::kTileBytes + j * 256);
       }
     }
     if (lookup) {
@@ -361,14 +389,11 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
   // ---- this lane's rows, and the queries as the first product's other operand
   constexpr int kQRegs = F::kBits == 32 ? D / 16 : F::kSteps;
   int t_of[NC];
-  bool live[NC];
   u32x4 qf[NC][kQRegs];
   float col_scale[NC], q_sum[NC];  // logit = (products) * col_scale; q_sum: the lowest value's factor
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
-    const int r = row0 + c * 16 + col;
-    live[c] = r < rows;
-    const int rr = live[c] ? r : rows - 1;
+    const int rr = min(row0 + (row_wave * NC + c) * 16 + col, rows - 1);
     const int t = p.blocks ? t_list : rr / p.G, head = h * p.G + (p.blocks ? rr : rr - t * p.G);
     t_of[c] = t;
     const char* q = p.q + ((size_t)b * p.q_stride[0] + (size_t)head * p.q_stride[1] + (size_t)t * p.q_stride[2]) * (format_bits(p.q_dtype) / 8);
@@ -425,20 +450,27 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
     for (int d = 0; d < F::kDTiles; ++d) o[c][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  for (int tile = tile0; tile < tile1; ++tile) {
-    const int k0 = tile * kTile;
-    if (tile + F::kStages - 1 < tile1) {
+  for (int turn = 0; turn < (RW > 1 ? per_group : tile1 - tile0); ++turn) {
+    const int tile = tile0 + turn, k0 = tile * kTile;
+    if constexpr (RW > 1) {
+      // behind the barrier the group's copies of this tile are all done, and so are its reads of the one before
+      wait_copies<0>();
+      wait_reads();
+      __syncthreads();
+      if (tile + 1 < tile1) issue(tile + 1);
+      if (tile >= tile1) continue;  // (the last group may have a tile less)
+    } else if (tile + F::kStages - 1 < tile1) {
       wait_reads();  // (of the stage that is filled again)
       issue(tile + F::kStages - 1);
       wait_copies<(F::kStages - 1) * kCopies>();
     } else {
       wait_copies<0>();
     }
-    const char* kt = own + (tile - tile0) % F::kStages * F::kStage;
+    const char* kt = own + turn % F::kStages * F::kStage;
     const char* vt = kt + F::kTileBytes;
     const float* kp = (const float*)(kt + 2 * F::kTileBytes);  // [parameter][K, V][key]
     const float* vp = kp + kTile;
-    const bool look = lookup ? (looks >> ((tile - tile0) & 31)) & 1 : k0 + kTile > first_new;
+    const bool look = lookup ? (looks >> (turn & 31)) & 1 : k0 + kTile > first_new;
 
     // ---- logits, but for the row's factor
     f32x4 s[NC][U];
@@ -475,20 +507,40 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
             s[c][u][r] = FORMAT == KVCRUSH_I4 ? __builtin_fmaf(s[c][u][r], scale[r], low[r] * q_sum[c]) : s[c][u][r] * scale[r];
       }
     }
-    uint32_t seen[NC];  // bit 4 u + r: this row sees the key
-#pragma unroll
-    for (int c = 0; c < NC; ++c) seen[c] = 0xFFFFu;
+    uint32_t seen[NC] = {};  // bit 4 u + r: this row sees the key (where it is looked at)
     if (look) {
+      // Which keys of the tile are there, and which rows see those of them that are new: bit k is key k.
+      int pos;
+      const uint64_t there = __ballot(slots.position(k0 + (lane & (kTile - 1)), pos)) & (~0ull >> (64 - kTile));
+      const int draft = pos - first_new;  // of key `lane`: number of the new token, negative for an older one
+      const uint64_t old = __ballot(draft < 0);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const uint64_t* words = p.mask ? p.mask + (size_t)b * p.mask_stride + (size_t)t_of[c] * p.mask_words : nullptr;
-        for (int i = 0; i < 4 * U; ++i) {
-          int pos;
-          bool see = slots.position(k0 + step_key(g, i), pos) && t_of[c] < n;
-          const int draft = pos - first_new;
-          if (see && draft >= 0) see = words ? (words[draft >> 6] >> (draft & 63)) & 1 : draft <= t_of[c];
-          if (!see) seen[c] &= ~(1u << i);
+        const int last = p.mask_words - 1;
+        uint64_t see = 0;
+        if (!slots.list) {  // the tile's new tokens are neighbours
+          const int d0 = k0 - first_new, up = max(-d0, 0), from = max(d0, 0);  // key `up` is new token `from`
+          if (words) {
+            const int w = from >> 6, s0 = from & 63;
+            const uint64_t a = words[min(w, last)], next = words[min(w + 1, last)];
+            see = (a >> s0) | ((next << 1) << (63 - s0));
+          } else {
+            const int most = t_of[c] - from;
+            see = most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
+          }
+          see = up >= 64 ? 0 : see << up;
+        } else {
+#pragma unroll 1
+          for (int k = 0; k < kTile; ++k) {
+            const int d = __builtin_amdgcn_readlane(draft, k);
+            const bool bit = words ? (words[min(max(d >> 6, 0), last)] >> (d & 63)) & 1 : d <= t_of[c];
+            see |= (uint64_t)bit << k;
+          }
         }
+        see = t_of[c] < n ? (see | old) & there : 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) seen[c] |= (uint32_t)(see >> (16 * u + 4 * g) & 15) << (4 * u);
       }
     }
 
@@ -557,21 +609,19 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
     }
     if constexpr (FORMAT != KVCRUSH_I8 && FORMAT != KVCRUSH_I4) {
       if (look) {
-        // A value that is not finite must not reach the rows that do not see its key (0 x NaN): such keys are
-        // added one by one, to the rows that do, and taken out of the tile.
-        uint32_t bad = 0;
+        // A value that is not finite must not reach the rows that do not see its key (0 x NaN): the keys of a tile
+        // with one are added one by one, each to the rows that see it.
+        bool odd = false;
 #pragma unroll
         for (int j = 0; j < F::kLoads; ++j) {
           const u32x4 x = *(const u32x4*)(vt + j * 1024 + lane * 16);
-          bool odd = false;
 #pragma unroll
           for (int i = 0; i < 4; ++i) odd = odd || !all_finite<FORMAT>(x[i]);
-          if (odd) bad |= 1u << (in_tile[j] / F::kRow);
         }
-        bad = kvc::wave_reduce(bad, 0u, [](uint32_t x, uint32_t y) { return x | y; });
-        if (bad) {
-          for (uint32_t left = bad; left; left &= left - 1) {
-            const int key = __builtin_ctz(left), reg = 4 * (key >> 4) + (key & 3), from = col + 16 * ((key >> 2) & 3);
+        if (__ballot(odd) != 0) {
+#pragma unroll 1
+          for (int key = 0; key < kTile; ++key) {
+            const int reg = 4 * (key >> 4) + (key & 3), from = col + 16 * ((key >> 2) & 3);
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
               float x = 0.0f;
@@ -580,17 +630,15 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
               x = __shfl(x, from);
               if (__shfl((int)((seen[c] >> reg) & 1), from)) {
 #pragma unroll
-                for (int d = 0; d < F::kDTiles; ++d)
+                for (int d = 0; d < F::kDTiles; ++d) {
 #pragma unroll
                   for (int r = 0; r < 4; ++r) o[c][d][r] += x * tile_value<F>(vt, key, d * 16 + 4 * g + r);
+                  asm volatile("" : : : "memory");  // (few values at a time: no registers for what is rare)
+                }
               }
             }
           }
-          kvc::wave_fence();
-#pragma unroll
-          for (int j = 0; j < F::kLoads; ++j)
-            if ((bad >> (in_tile[j] / F::kRow)) & 1) *(u32x4*)(const_cast<char*>(vt) + j * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-          kvc::wave_fence();
+          continue;
         }
       }
     }
@@ -631,7 +679,7 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
             yh = (float)f[1];
           }
           hi[c][i / 4][i % 4] = both;
-          lo[c][i / 4][i % 4] = pack2<P>(x - xh, y - yh);
+          lo[c][i / 4][i % 4] = pack2<P>(__builtin_fmaf(xh, -1.0f, x), __builtin_fmaf(yh, -1.0f, y));
         }
 #pragma unroll
       for (int d = 0; d < F::kDTiles; ++d) {
@@ -657,7 +705,7 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
   // ---- the waves' rows are brought to one reference and added up
   constexpr int kPitch = D + 4;
   float2* ml = (float2*)lds_all;                                    // [waves][NC][16]
-  float* sums = (float*)(lds_all + kWaves * NC * 128);           // [waves][16][kPitch]
+  float* sums = (float*)(lds_all + kWaves * NC * 128);              // [waves][16][kPitch]
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     l[c] = row_sum(l[c]);
@@ -682,7 +730,7 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
   for (int c = 0; c < NC; ++c) {
     float top = kNegBig;
 #pragma unroll
-    for (int x = 0; x < kWaves; ++x) top = fmaxf(top, ml[(x * NC + c) * 16 + col].x);
+    for (int x = 0; x < kGroups; ++x) top = fmaxf(top, ml[((x * RW + row_wave) * NC + c) * 16 + col].x);
     const float a = __builtin_amdgcn_exp2f(m[c] - top);
     if (c > 0) __syncthreads();
 #pragma unroll
@@ -690,19 +738,20 @@ __global__ __launch_bounds__(F::waves(NC) * KVC_WAVE) void attend_kernel(AttendP
       *(f32x4*)(sums + (wave * 16 + col) * kPitch + d * 16 + 4 * g) = f32x4{o[c][d][0] * a, o[c][d][1] * a, o[c][d][2] * a, o[c][d][3] * a};
     __syncthreads();
     // four values a thread
-    for (int i = tid; i < 16 * (D / 4); i += kWaves * KVC_WAVE) {
-      const int row = i / (D / 4), e = i % (D / 4) * 4, r = row0 + c * 16 + row;
+    for (int i = tid; i < RW * 16 * (D / 4); i += kWaves * KVC_WAVE) {
+      const int of = i / (16 * (D / 4)), row = i / (D / 4) % 16, e = i % (D / 4) * 4;  // (of: the row wave)
+      const int r = row0 + (of * NC + c) * 16 + row;
       if (r >= rows) break;  // (rows ascend with i)
       const int t = p.blocks ? t_list : r / p.G, head = h * p.G + (p.blocks ? r : r - t * p.G);
       float most = kNegBig, total = 0.0f;
 #pragma unroll
-      for (int x = 0; x < kWaves; ++x) most = fmaxf(most, ml[(x * NC + c) * 16 + row].x);
+      for (int x = 0; x < kGroups; ++x) most = fmaxf(most, ml[((x * RW + of) * NC + c) * 16 + row].x);
       f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int x = 0; x < kWaves; ++x) {
-        const float2 y = ml[(x * NC + c) * 16 + row];
+      for (int x = 0; x < kGroups; ++x) {
+        const float2 y = ml[((x * RW + of) * NC + c) * 16 + row];
         total += y.y * __builtin_amdgcn_exp2f(y.x - most);
-        sum += *(const f32x4*)(sums + (x * 16 + row) * kPitch + e);
+        sum += *(const f32x4*)(sums + ((x * RW + of) * 16 + row) * kPitch + e);
       }
       const size_t at = ((size_t)b * p.Hq + head) * p.T + t;
       if (p.n_split > 1) {
@@ -754,7 +803,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
 
 // ------------------------------------------------------------------------------------ host
 struct Plan {
-  int G, NC, row_tiles, n_split;
+  int G, NC, RW, row_tiles, n_split;
   long long rows;  // B * Hq * T
 };
 
@@ -773,8 +822,12 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   plan.G = a->Hq / c->Hkv;
   plan.rows = (long long)c->B * a->Hq * a->T;
   const long long r = a->blocks ? plan.G : (long long)plan.G * a->T;
-  plan.NC = r > 32 ? 4 : r > 16 ? 2 : 1;
-  const long long tiles = (r + 16 * plan.NC - 1) / (16 * plan.NC) * (a->blocks ? a->T : 1);
+  // Rows of a workgroup: 16 or 32 if they are no more; otherwise 64 or 128 that share their tiles, whichever leaves fewer
+  // places empty (128 if both leave as many: the keys are read half as often).
+  plan.NC = r > 16 ? 2 : 1;
+  plan.RW = r <= 32 ? 1 : (r + 127) / 128 * 2 > (r + 63) / 64 ? 2 : 4;
+  const int rows = 16 * plan.NC * plan.RW;
+  const long long tiles = (r + rows - 1) / rows * (a->blocks ? a->T : 1);
   plan.row_tiles = (int)tiles;
   const long long keys = a->blocks ? std::min<long long>((long long)a->n_list * a->unit, c->capacity) : c->S;
   const long long base = (long long)c->B * c->Hkv * tiles;
@@ -789,22 +842,22 @@ size_t plan_bytes(const Plan& p, int D) {
   return p.n_split == 1 ? 0 : ml_bytes(p) + (size_t)p.rows * p.n_split * D * sizeof(float);
 }
 
-template <class F, int NC>
+template <class F, int NC, int RW>
 kvcrush_status launch_attend(const AttendParams& p, hipStream_t stream) {
-  constexpr int kWaves = F::waves(NC);
-  constexpr int kLoop = kWaves * (F::kStages * F::kStage + kAhead * 4);
-  constexpr int kEnd = kWaves * (NC * 128 + 16 * (F::D + 4) * 4);
+  constexpr int kWaves = F::waves(NC, RW);
+  constexpr int kLoop = F::lds(kWaves, RW), kEnd = kWaves * (NC * 128 + 16 * (F::D + 4) * 4);
   constexpr int kLds = kLoop > kEnd ? kLoop : kEnd;
   static_assert(kLds <= kvc::kLdsPerWorkgroup, "LDS of a workgroup");
-  kvcrush_status st = kvc::allow_large_lds<attend_kernel<F, NC>>(0);
+  kvcrush_status st = kvc::allow_large_lds<attend_kernel<F, NC, RW>>(0);
   if (st != KVCRUSH_OK) return st;
   const dim3 grid((unsigned)((p.groups + 7) / 8 * 8) * p.row_tiles);
-  return kvc::launch(attend_kernel<F, NC>, grid, dim3(kWaves * KVC_WAVE), kLds, stream, p);
+  return kvc::launch(attend_kernel<F, NC, RW>, grid, dim3(kWaves * KVC_WAVE), kLds, stream, p);
 }
 
 template <class F>
-kvcrush_status launch_rows(const AttendParams& p, int NC, hipStream_t stream) {
-  return NC == 4 ? launch_attend<F, 4>(p, stream) : NC == 2 ? launch_attend<F, 2>(p, stream) : launch_attend<F, 1>(p, stream);
+kvcrush_status launch_rows(const AttendParams& p, const Plan& plan, hipStream_t stream) {
+  if (plan.NC == 1) return launch_attend<F, 1, 1>(p, stream);
+  return plan.RW == 1 ? launch_attend<F, 2, 1>(p, stream) : plan.RW == 2 ? launch_attend<F, 2, 2>(p, stream) : launch_attend<F, 2, 4>(p, stream);
 }
 
 }  // namespace
@@ -853,7 +906,7 @@ extern "C" kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcru
   hipStream_t stream = (hipStream_t)hip_stream;
   st = with_format(cache->format, [&](auto fmt) -> kvcrush_status {
     constexpr int FMT = decltype(fmt)::value;
-    return D == 128 ? launch_rows<Fmt<FMT, 128>>(p, plan.NC, stream) : launch_rows<Fmt<FMT, 64>>(p, plan.NC, stream);
+    return D == 128 ? launch_rows<Fmt<FMT, 128>>(p, plan, stream) : launch_rows<Fmt<FMT, 64>>(p, plan, stream);
   });
   if (st != KVCRUSH_OK || plan.n_split == 1) return st;
   const dim3 grid((unsigned)plan.rows);

@@ -32,8 +32,8 @@ struct View {
 
   __device__ int length(int b) const { return lengths ? min(max(lengths[b], 0), S) : S; }
   // Token `pos` of sequence b as the pool or the sequence counts tokens (a block outside the pool is pulled into it).
-  __device__ int token(int b, int pos) const {
-    if (!table) return pos;
+  __device__ int token(int b, int pos) const { return table ? paged_token(b, pos) : pos; }
+  __device__ int paged_token(int b, int pos) const {
     const int block = min(max(table[(size_t)b * table_width + pos / block_size], 0), n_blocks - 1);
     return block * block_size + pos % block_size;
   }
@@ -130,8 +130,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const f32x2 f = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
   } else {
-    const f16x2 h = {(_Float16)a, (_Float16)b};
-    return __builtin_bit_cast(uint32_t, h);
+    const f32x2 f = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, f16x2));
   }
 }
 
