@@ -35,15 +35,18 @@ struct AttendParams {
   const char* q;
   char* out;
   float* lse;
-  float* part_o;   // workspace [B * Hq * T][n_split][D]
-  float2* part_ml;  // workspace [B * Hq * T][n_split]
+  float* part_o;   // workspace [Hkv][pieces][T * G][D]
+  float2* part_ml;  // workspace [Hkv][pieces][T * G]
+  int2* cuts;       // workspace [64]: first piece and number of pieces of each sequence, where they are dealt by length
   const uint64_t* mask;
   const int32_t* n_new;
   const int32_t* blocks;
   int64_t q_stride[3], out_stride[3];  // elements
   int64_t mask_stride;
-  int Hq, G, T, n_split, n_list, unit, mask_words, q_dtype;
-  int row_tiles, groups;  // workgroups that share a sequence's piece; pieces of all sequences and KV heads
+  int Hq, G, T, n_list, unit, mask_words, q_dtype;
+  int pieces;     // of all sequences together, per KV head
+  int n_split;    // pieces of each sequence; 0: they are dealt by length
+  int row_tiles;  // workgroups that share a piece
   float scale_log2;
 };
 
@@ -62,10 +65,11 @@ struct Fmt {
   static constexpr int kParam = kQuant ? (FORMAT == KVCRUSH_I4 ? 2 : 1) : 0;  // floats beside a row
   static constexpr int kParamLoads = kParam * 2 * kTile / 64;                 // of 4 bytes a lane
   static constexpr int kStage = 2 * kTileBytes + kParamLoads * 256;
-  static constexpr int kStages = 2;
   // Eight waves where LDS and registers have room for them: two to a SIMD, so that one's matrix instructions run beside
   // the other's arithmetic.  RW of them share a tile.
-  static constexpr int lds(int waves, int RW) { return waves / RW * kStages * kStage + waves * kAhead * 4; }
+  static constexpr int lds(int waves, int RW) { return waves / RW * stages(RW) * kStage + waves * kAhead * 4; }
+  // Groups of waves that meet at a barrier look two tiles ahead where there is room.
+  static constexpr int stages(int RW) { return RW > 1 && 8 / RW * 3 * kStage + 8 * kAhead * 4 <= kvc::kLdsPerWorkgroup ? 3 : 2; }
   static constexpr int waves(int NC, int RW) {
     return (NC == 2 && kBits == 4) || lds(8, RW) > kvc::kLdsPerWorkgroup ? 4 : 8;
   }
@@ -229,13 +233,13 @@ struct Slots {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy16(const char* from, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(dst), "v"(from) : "m0", "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(from) : "m0", "memory");
 }
 __device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t dst) {  // base uniform
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(off), "s"(base) : "m0", "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ void copy4(const char* from, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(dst), "v"(from) : "m0", "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(from) : "m0", "memory");
 }
 #pragma clang diagnostic pop
 template <int LEFT>
@@ -261,12 +265,40 @@ __device__ __forceinline__ void store_result(const AttendParams& p, int b, int h
     *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_F16>(x[0], x[1]), pack2<KVCRUSH_F16>(x[2], x[3])};
 }
 
+// The cut of the sequences' keys into p.pieces pieces of `size` steps of `step` keys, in order of the sequences, each with
+// one piece at least: the smallest size (but for a sixteenth) with which they suffice.  Whole waves; B <= 64.
+struct Deal {
+  int size;         // steps of a piece
+  int first, n;     // of sequence `lane`
+  int total;
+};
+__device__ __forceinline__ Deal deal(const AttendParams& p, int step) {
+  const int lane = kvc::lane_id();
+  const int steps = lane < p.c.B ? (p.c.length(lane) + step - 1) / step : 0;
+  auto sum = [](int v) { return (int)kvc::wave_reduce((uint32_t)v, 0u, [](uint32_t a, uint32_t b) { return a + b; }); };
+  Deal d;
+  d.size = max((sum(steps) + p.pieces - 1) / p.pieces, 1);
+  for (;; d.size += max(d.size >> 4, 1)) {
+    d.n = lane < p.c.B ? max((steps + d.size - 1) / d.size, 1) : 0;
+    d.total = sum(d.n);
+    if (d.total <= p.pieces) break;  // (pieces >= B: with one piece each at the latest)
+  }
+  int end = d.n;
+#pragma unroll
+  for (int off = 1; off < KVC_WAVE; off *= 2) {
+    const int o = __shfl_up(end, off);
+    if (lane >= off) end += o;
+  }
+  d.first = end - d.n;
+  return d;
+}
+
 // RW: waves that share a tile, each with 16 NC rows of its own.  One: the waves are on their own, and nobody waits for
 // another's copies.  More: they copy a share each and meet at a barrier per tile, so that many rows cost one reading of
 // the keys.
 template <class F, int NC, int RW>
 __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(AttendParams p) {
-  constexpr int kWaves = F::waves(NC, RW), kGroups = kWaves / RW;
+  constexpr int kWaves = F::waves(NC, RW), kGroups = kWaves / RW, kStages = F::stages(RW);
   constexpr int D = F::D, FORMAT = F::FORMAT, kTile = F::kTile, U = F::kSub;
   extern __shared__ __attribute__((aligned(1024))) char lds_all[];
   const int tid = threadIdx.x, lane = kvc::lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / KVC_WAVE);
@@ -274,9 +306,23 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   // Workgroups with numbers 8 apart run on one chiplet, one after the other: the row tiles of a piece, which read the same
   // keys, are put there side by side.
   const int xcd = blockIdx.x & 7, place = blockIdx.x >> 3, row_tile = place % p.row_tiles;
-  const int group = place / p.row_tiles * 8 + xcd;
-  if (group >= p.groups) return;
-  const int bh = group / p.n_split, split = group - bh * p.n_split, b = bh / p.c.Hkv, h = bh - b * p.c.Hkv;
+  const int group = place / p.row_tiles * 8 + xcd, h = group / p.pieces, piece = group - h * p.pieces;
+  if (h >= p.c.Hkv) return;
+  int b, split, n_split, piece_tiles = 0;  // this piece of the n_split of sequence b
+  if (p.n_split > 0) {
+    n_split = p.n_split;
+    b = piece / n_split;
+    split = piece - b * n_split;
+  } else {
+    const Deal d = deal(p, F::kTile * kGroups);
+    if (piece >= d.total) return;
+    b = 63 - __builtin_clzll(__ballot(lane < p.c.B && d.first <= piece));
+    split = piece - __builtin_amdgcn_readlane(d.first, b);
+    n_split = __builtin_amdgcn_readlane(d.n, b);
+    piece_tiles = d.size * kGroups;
+    if (blockIdx.x == 0 && tid < p.c.B) p.cuts[tid] = make_int2(d.first, d.n);
+  }
+  const int bh = b * p.c.Hkv + h;
   const int L = p.c.length(b), n = new_tokens(p.n_new, b, p.T, L);
   // with lists, a query's G heads are the rows
   constexpr int kRows = 16 * NC * RW;
@@ -292,16 +338,17 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   slots.L = L;
 
   // this wave's (or its group's) tiles: a contiguous piece of the workgroup's
-  const int tiles = (slots.n + kTile - 1) / kTile, per_wg = (tiles + p.n_split - 1) / p.n_split;
+  const int tiles = (slots.n + kTile - 1) / kTile, per_wg = piece_tiles > 0 ? piece_tiles : (tiles + n_split - 1) / n_split;
   const int wg0 = min(split * per_wg, tiles), wg1 = min(wg0 + per_wg, tiles);
   const int per_group = (wg1 - wg0 + kGroups - 1) / kGroups;
-  const int tile0 = min(wg0 + key_group * per_group, wg1), tile1 = min(tile0 + per_group, wg1);
+  const int tile0 = __builtin_amdgcn_readfirstlane(min(wg0 + key_group * per_group, wg1));
+  const int tile1 = __builtin_amdgcn_readfirstlane(min(tile0 + per_group, wg1));
 
   // ---- copies of tiles into this group's stages
-  char* own = lds_all + key_group * (F::kStages * F::kStage);
+  char* own = lds_all + key_group * (kStages * F::kStage);
   const uint32_t own_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)own);
   // token of each slot (a table of each wave's own); bit 31: the slot has to be looked at
-  int* places = (int*)(lds_all + kGroups * F::kStages * F::kStage) + wave * kAhead;
+  int* places = (int*)(lds_all + kGroups * kStages * F::kStage) + wave * kAhead;
   const size_t row_base = p.c.base(b, h), row_step = p.c.step();
   const bool lookup = p.c.table || p.blocks;
   const int first_new = L - n;
@@ -320,7 +367,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   constexpr int kCopies = kOwn + F::kParamLoads;
   auto issue = [&](int tile) {
     const int k0 = tile * kTile, i = tile - tile0, ahead = (i * kTile) & (kAhead - 1);
-    const uint32_t stage = own_at + (i % F::kStages) * F::kStage, dst = stage + row_wave * 1024;
+    const uint32_t stage = own_at + (i % kStages) * F::kStage, dst = stage + row_wave * 1024;
     if (lookup && ahead == 0) {
       // (branches only around the loops, so that a loop's loads are all on their way before the first is used)
       constexpr int kEach = kAhead / KVC_WAVE;
@@ -383,7 +430,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     }
   };
 #pragma unroll
-  for (int i = 0; i < F::kStages - 1; ++i)
+  for (int i = 0; i < (RW > 1 ? kStages - 1 : kStages); ++i)
     if (tile0 + i < tile1) issue(tile0 + i);
 
   // ---- this lane's rows, and the queries as the first product's other operand
@@ -397,7 +444,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     const int t = p.blocks ? t_list : rr / p.G, head = h * p.G + (p.blocks ? rr : rr - t * p.G);
     t_of[c] = t;
     const char* q = p.q + ((size_t)b * p.q_stride[0] + (size_t)head * p.q_stride[1] + (size_t)t * p.q_stride[2]) * (format_bits(p.q_dtype) / 8);
-    col_scale[c] = p.scale_log2;
+    col_scale[c] = fmaxf(p.scale_log2, 0x1p-100f);  // (never zero: what a row does not see is -infinity times this)
     q_sum[c] = 0.0f;
     if constexpr (!F::kQuant) {
 #pragma unroll
@@ -426,7 +473,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
       const int up = min(141 - (int)(top >> 23), 126);  // >= -114
       const float by = __builtin_amdgcn_ldexpf(1.0f, up);
       q_sum[c] *= by;
-      col_scale[c] = p.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, -up);
+      col_scale[c] = fmaxf(p.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, -up), 0x1p-120f);
       constexpr int kOrder[2][8] = {{0, 1, 2, 3, 4, 5, 6, 7}, {0, 4, 1, 5, 2, 6, 3, 7}};
       constexpr int o = FORMAT == KVCRUSH_I4 ? 1 : 0;
 #pragma unroll
@@ -439,8 +486,9 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
 
   f32x4 o[NC][F::kDTiles];
   // Reference exponent m (base 2) of a row: o, l and z are sums of 2^(logit - m).  It need not be the largest logit: it is
-  // raised, and the sums brought to it, only when a product of probability and V's scale passes 2^8 (or, where scales are
-  // tiny, a probability passes 2^96), so that what is rounded to 16 bits lies in their range and few tiles pay for it.
+  // raised, and the sums brought to it, only where a product of probability and V's scale could pass 2^8 (scales below
+  // 2^-88 counting as that, so that no probability passes 2^96): what is rounded to 16 bits lies in their range, and few
+  // tiles pay for it.
   float m[NC], l[NC], z[NC];  // l: sum of this lane's keys; z: sum of probability x lowest value
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -454,19 +502,25 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     const int tile = tile0 + turn, k0 = tile * kTile;
     if constexpr (RW > 1) {
       // behind the barrier the group's copies of this tile are all done, and so are its reads of the one before
-      wait_copies<0>();
+      if (kStages == 3 && tile + 1 < tile1)
+        wait_copies<kCopies>();
+      else
+        wait_copies<0>();
       wait_reads();
       __syncthreads();
-      if (tile + 1 < tile1) issue(tile + 1);
+      if (tile + kStages - 1 < tile1) issue(tile + kStages - 1);
       if (tile >= tile1) continue;  // (the last group may have a tile less)
-    } else if (tile + F::kStages - 1 < tile1) {
-      wait_reads();  // (of the stage that is filled again)
-      issue(tile + F::kStages - 1);
-      wait_copies<(F::kStages - 1) * kCopies>();
     } else {
-      wait_copies<0>();
+      if (turn > 0) {
+        wait_reads();  // (of the stage that is filled again)
+        if (tile + kStages - 1 < tile1) issue(tile + kStages - 1);
+      }
+      if (tile + 1 < tile1)
+        wait_copies<kCopies>();
+      else
+        wait_copies<0>();
     }
-    const char* kt = own + turn % F::kStages * F::kStage;
+    const char* kt = own + turn % kStages * F::kStage;
     const char* vt = kt + F::kTileBytes;
     const float* kp = (const float*)(kt + 2 * F::kTileBytes);  // [parameter][K, V][key]
     const float* vp = kp + kTile;
@@ -507,6 +561,21 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
             s[c][u][r] = FORMAT == KVCRUSH_I4 ? __builtin_fmaf(s[c][u][r], scale[r], low[r] * q_sum[c]) : s[c][u][r] * scale[r];
       }
     }
+    f32x4 v_scale[U], v_low[U];
+    float above[NC];  // log2 of the largest scale of V that this lane's keys have, -88 at least
+    if constexpr (F::kQuant) {
+      float top = 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v_scale[u] = *(const f32x4*)(vp + 16 * u + 4 * g);
+        if constexpr (FORMAT == KVCRUSH_I4) v_low[u] = *(const f32x4*)(vp + 2 * kTile + 16 * u + 4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, v_scale[u][r]);
+      }
+      top = fmaxf(__builtin_amdgcn_logf(top), -88.0f);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) above[c] = top;
+    }
     uint32_t seen[NC] = {};  // bit 4 u + r: this row sees the key (where it is looked at)
     if (look) {
       // Which keys of the tile are there, and which rows see those of them that are new: bit k is key k.
@@ -541,54 +610,27 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         see = t_of[c] < n ? (see | old) & there : 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) seen[c] |= (uint32_t)(see >> (16 * u + 4 * g) & 15) << (4 * u);
+        // (a logit or a scale that the row does not see may be anything)
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4 * U; ++i) {
+          const bool it = (seen[c] >> i) & 1;
+          s[c][i / 4][i % 4] = it ? s[c][i / 4][i % 4] : -__builtin_inff();
+          if constexpr (F::kQuant) top = fmaxf(top, it ? v_scale[i / 4][i % 4] : 0.0f);
+        }
+        if constexpr (F::kQuant) above[c] = fmaxf(__builtin_amdgcn_logf(top), -88.0f);
       }
     }
 
     // ---- probabilities, times V's scale
-    f32x4 v_scale[U], v_low[U];
-    if constexpr (F::kQuant) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        v_scale[u] = *(const f32x4*)(vp + 16 * u + 4 * g);
-        if constexpr (FORMAT == KVCRUSH_I4) v_low[u] = *(const f32x4*)(vp + 2 * kTile + 16 * u + 4 * g);
-      }
-    }
-    f32x4 w[NC][U];
-    auto weigh = [&](int c, f32x4 (&pr)[U]) {  // pr: probabilities, w: times scales
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          pr[u][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][u][r], col_scale[c], -m[c]));
-          if constexpr (F::kQuant)
-            w[c][u][r] = pr[u][r] * v_scale[u][r];
-          else
-            w[c][u][r] = pr[u][r];
-        }
-      if (look) {  // (a logit or a scale that the row does not see may be anything)
-#pragma unroll
-        for (int i = 0; i < 4 * U; ++i)
-          if (!((seen[c] >> i) & 1)) pr[i / 4][i % 4] = w[c][i / 4][i % 4] = 0.0f;
-      }
-    };
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      f32x4 pr[U];
-      weigh(c, pr);
-      float wide = w[c][0][0], top = pr[0][0];
+      float most = s[c][0][0];
 #pragma unroll
-      for (int i = 1; i < 4 * U; ++i) {
-        wide = fmaxf(wide, w[c][i / 4][i % 4]);
-        if constexpr (F::kQuant) top = fmaxf(top, pr[i / 4][i % 4]);
-      }
-      if (__ballot(wide > 0x1p8f || (F::kQuant && top > 0x1p96f)) != 0) {
-        float most = kNegBig;
-#pragma unroll
-        for (int i = 0; i < 4 * U; ++i) {
-          float x = s[c][i / 4][i % 4] * col_scale[c];
-          if constexpr (F::kQuant) x = fmaxf(x + __builtin_amdgcn_logf(v_scale[i / 4][i % 4]), x - 96.0f);
-          if (!look || ((seen[c] >> i) & 1)) most = fmaxf(most, x);
-        }
+      for (int i = 1; i < 4 * U; ++i) most = fmaxf(most, s[c][i / 4][i % 4]);
+      most *= col_scale[c];
+      if constexpr (F::kQuant) most += above[c];
+      if (__ballot(most - m[c] > 8.0f) != 0) {
         const float mn = fmaxf(m[c], row_max(most)), a = __builtin_amdgcn_exp2f(m[c] - mn);
         m[c] = mn;
         l[c] *= a;
@@ -597,13 +639,29 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         for (int d = 0; d < F::kDTiles; ++d)
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[c][d][r] *= a;
-        weigh(c, pr);
       }
+      f32x4 pr[U];
 #pragma unroll
       for (int i = 0; i < 4 * U; ++i) {
+        pr[i / 4][i % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][i / 4][i % 4], col_scale[c], -m[c]));
         l[c] += pr[i / 4][i % 4];
-        if constexpr (FORMAT == KVCRUSH_I4) {
-          if (!look || ((seen[c] >> i) & 1)) z[c] = __builtin_fmaf(pr[i / 4][i % 4], v_low[i / 4][i % 4], z[c]);
+        if constexpr (F::kQuant)
+          s[c][i / 4][i % 4] = pr[i / 4][i % 4] * v_scale[i / 4][i % 4];
+        else
+          s[c][i / 4][i % 4] = pr[i / 4][i % 4];
+      }
+      if constexpr (F::kQuant) {
+        if (look) {
+          asm volatile("");  // (a branch, not selections that every tile would pay for)
+#pragma unroll
+          for (int i = 0; i < 4 * U; ++i) {
+            const bool it = (seen[c] >> i) & 1;
+            s[c][i / 4][i % 4] = it ? s[c][i / 4][i % 4] : 0.0f;
+            if constexpr (FORMAT == KVCRUSH_I4) z[c] = it ? __builtin_fmaf(pr[i / 4][i % 4], v_low[i / 4][i % 4], z[c]) : z[c];
+          }
+        } else if constexpr (FORMAT == KVCRUSH_I4) {
+#pragma unroll
+          for (int i = 0; i < 4 * U; ++i) z[c] = __builtin_fmaf(pr[i / 4][i % 4], v_low[i / 4][i % 4], z[c]);
         }
       }
     }
@@ -626,7 +684,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
             for (int c = 0; c < NC; ++c) {
               float x = 0.0f;
 #pragma unroll
-              for (int i = 0; i < 4 * U; ++i) x = i == reg ? w[c][i / 4][i % 4] : x;
+              for (int i = 0; i < 4 * U; ++i) x = i == reg ? s[c][i / 4][i % 4] : x;
               x = __shfl(x, from);
               if (__shfl((int)((seen[c] >> reg) & 1), from)) {
 #pragma unroll
@@ -652,7 +710,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
           const int e = d * 16 + col;  // value
           const float v = *(const float*)(vt + F::chunk_at(4 * g + r, e >> 2) + (e & 3) * 4);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, w[c][0][r], o[c][d], 0, 0, 0);
+          for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[c][0][r], o[c][d], 0, 0, 0);
         }
       }
     } else {
@@ -664,7 +722,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 2 * U; ++i) {
-          float x = w[c][i / 2][2 * (i % 2)], y = w[c][i / 2][2 * (i % 2) + 1];
+          float x = s[c][i / 2][2 * (i % 2)], y = s[c][i / 2][2 * (i % 2) + 1];
           // (values from here on: otherwise the compiler may round the product behind x to 16 bits in one step for
           // `hi` and in two for what `hi` left)
           asm("" : "+v"(x), "+v"(y));
@@ -753,10 +811,10 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         total += y.y * __builtin_amdgcn_exp2f(y.x - most);
         sum += *(const f32x4*)(sums + ((x * RW + of) * 16 + row) * kPitch + e);
       }
-      const size_t at = ((size_t)b * p.Hq + head) * p.T + t;
-      if (p.n_split > 1) {
-        if (e == 0) p.part_ml[at * p.n_split + split] = make_float2(most, total);
-        *(f32x4*)(p.part_o + (at * p.n_split + split) * D + e) = sum;
+      if (n_split > 1) {
+        const size_t at = ((size_t)h * p.pieces + piece) * (p.T * p.G) + t * p.G + (head - h * p.G);
+        if (e == 0) p.part_ml[at] = make_float2(most, total);
+        *(f32x4*)(p.part_o + at * D + e) = sum;
       } else {
         store_result(p, b, head, t, e, most, total, sum);
       }
@@ -772,14 +830,22 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
   __shared__ f32x4 sums[kGroups][kLanes];
   __shared__ float2 mls[kGroups];
   const int row = blockIdx.x, part = threadIdx.x / kLanes, e = threadIdx.x % kLanes * 4;  // row = (b * Hq + head) * T + t
-  const float2* ml = p.part_ml + (size_t)row * p.n_split;
-  const float* o = p.part_o + (size_t)row * p.n_split * D + e;
+  const int t = row % p.T, head = row / p.T % p.Hq, b = row / p.T / p.Hq, h = head / p.G;
+  int first, n = p.n_split;
+  if (n > 0) {
+    first = b * n;
+  } else {
+    first = p.cuts[b].x;
+    n = p.cuts[b].y;
+    if (n == 1) return;  // (uniform: there already)
+  }
+  const size_t pitch = p.T * p.G, at = ((size_t)h * p.pieces + first) * pitch + t * p.G + (head - h * p.G);
   float m = kNegBig, total = 0.0f;
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-  for (int i = part; i < p.n_split; i += kGroups) {
-    const float2 x = ml[i];
-    const f32x4 y = *(const f32x4*)(o + (size_t)i * D);
+  for (int i = part; i < n; i += kGroups) {
+    const float2 x = p.part_ml[at + i * pitch];
+    const f32x4 y = *(const f32x4*)(p.part_o + (at + i * pitch) * D + e);
     const float mn = fmaxf(m, x.x), a = __builtin_amdgcn_exp2f(m - mn), c = __builtin_amdgcn_exp2f(x.x - mn);
     m = mn;
     total = total * a + x.y * c;
@@ -798,16 +864,17 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
     total = total * a + x.y * c;
     sum = sum * a + y * c;
   }
-  store_result(p, row / p.T / p.Hq, row / p.T % p.Hq, row % p.T, e, m, total, sum);
+  store_result(p, b, head, t, e, m, total, sum);
 }
 
 // ------------------------------------------------------------------------------------ host
 struct Plan {
-  int G, NC, RW, row_tiles, n_split;
+  int G, NC, RW, row_tiles, n_split, pieces;  // n_split 0: dealt by length
   long long rows;  // B * Hq * T
 };
 
-constexpr int kMaxSplit = 128;
+constexpr int kMaxSplit = 256;
+constexpr long long kUnits = 256;  // compute units of the chip
 
 kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, Plan& plan) {
   kvcrush_status st = check(c);
@@ -830,16 +897,36 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   const long long tiles = (r + rows - 1) / rows * (a->blocks ? a->T : 1);
   plan.row_tiles = (int)tiles;
   const long long keys = a->blocks ? std::min<long long>((long long)a->n_list * a->unit, c->capacity) : c->S;
-  const long long base = (long long)c->B * c->Hkv * tiles;
-  long long split = (256 + base - 1) / base;
-  split = std::min(split, (keys + 255) / 256);
-  plan.n_split = (int)std::max(1ll, std::min<long long>(split, kMaxSplit));
+  // One workgroup to a compute unit: as many pieces as leave the fewest keys to the unit that has most, fewer where that
+  // gains nothing.
+  const long long base = (long long)c->Hkv * tiles, most = std::max(1ll, std::min<long long>((keys + 255) / 256, kMaxSplit));
+  if (c->lengths && !a->blocks && c->B > 1 && c->B <= KVC_WAVE && base * c->B < kUnits) {
+    plan.n_split = 0;
+    plan.pieces = (int)std::max<long long>(c->B, std::min(kUnits / base, most * c->B));
+  } else {
+    plan.n_split = 1;
+    double least = 0.0;
+    for (int n = 1; n <= most; ++n) {
+      const double keys_of_unit = (double)((base * c->B * n + kUnits - 1) / kUnits) / n;
+      if (n > 1 && keys_of_unit > 0.95 * least) continue;
+      least = keys_of_unit;
+      plan.n_split = n;
+    }
+    plan.pieces = c->B * plan.n_split;
+  }
   return KVCRUSH_OK;
 }
 
-size_t ml_bytes(const Plan& p) { return kvc::align_up((size_t)p.rows * p.n_split * sizeof(float2), 256); }
-size_t plan_bytes(const Plan& p, int D) {
-  return p.n_split == 1 ? 0 : ml_bytes(p) + (size_t)p.rows * p.n_split * D * sizeof(float);
+constexpr size_t kCutBytes = KVC_WAVE * sizeof(int2);
+bool merged(const Plan& p) { return p.n_split != 1; }
+long long part_rows(const kvcrush_cache* c, const kvcrush_attend_args* a, const Plan& p) {
+  return (long long)a->Hq * a->T * p.pieces;
+}
+size_t ml_bytes(long long rows) { return kvc::align_up((size_t)rows * sizeof(float2), 256); }
+size_t plan_bytes(const kvcrush_cache* c, const kvcrush_attend_args* a, const Plan& p) {
+  if (!merged(p)) return 0;
+  const long long rows = part_rows(c, a, p);
+  return kCutBytes + ml_bytes(rows) + (size_t)rows * c->D * sizeof(float);
 }
 
 template <class F, int NC, int RW>
@@ -850,8 +937,10 @@ kvcrush_status launch_attend(const AttendParams& p, hipStream_t stream) {
   static_assert(kLds <= kvc::kLdsPerWorkgroup, "LDS of a workgroup");
   kvcrush_status st = kvc::allow_large_lds<attend_kernel<F, NC, RW>>(0);
   if (st != KVCRUSH_OK) return st;
-  const dim3 grid((unsigned)((p.groups + 7) / 8 * 8) * p.row_tiles);
-  return kvc::launch(attend_kernel<F, NC, RW>, grid, dim3(kWaves * KVC_WAVE), kLds, stream, p);
+  const dim3 grid((unsigned)((p.c.Hkv * p.pieces + 7) / 8 * 8) * p.row_tiles);
+  st = kvc::launch(attend_kernel<F, NC, RW>, grid, dim3(kWaves * KVC_WAVE), kLds, stream, p);
+  if (st != KVCRUSH_OK || p.n_split == 1) return st;
+  return kvc::launch(attend_merge_kernel<F::D>, dim3((unsigned)(p.c.B * p.Hq * p.T)), dim3(256), 0, stream, p);
 }
 
 template <class F>
@@ -864,7 +953,7 @@ kvcrush_status launch_rows(const AttendParams& p, const Plan& plan, hipStream_t 
 
 extern "C" size_t kvcrush_attend_workspace(const kvcrush_cache* cache, const kvcrush_attend_args* args) {
   Plan plan;
-  return make_plan(cache, args, plan) == KVCRUSH_OK ? plan_bytes(plan, cache->D) : 0;
+  return make_plan(cache, args, plan) == KVCRUSH_OK ? plan_bytes(cache, args, plan) : 0;
 }
 
 extern "C" kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcrush_attend_args* args, const void* q,
@@ -879,14 +968,15 @@ extern "C" kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcru
   if (!strides_ok(args->q_stride, args->Hq, args->T, D, elem, 0, p.q_stride) ||
       !strides_ok(args->out_stride, args->Hq, args->T, D, elem, D, p.out_stride))
     return KVCRUSH_ERR_INVALID_ARG;
-  const size_t need = plan_bytes(plan, D);
+  const size_t need = plan_bytes(cache, args, plan);
   if (need > 0 && (!workspace || !kvc::aligned16(workspace) || workspace_bytes < need)) return KVCRUSH_ERR_WORKSPACE;
   p.c = view(cache);
   p.q = (const char*)q;
   p.out = (char*)out;
   p.lse = lse;
-  p.part_ml = (float2*)workspace;
-  p.part_o = need > 0 ? (float*)((char*)workspace + ml_bytes(plan)) : nullptr;
+  p.cuts = (int2*)workspace;
+  p.part_ml = (float2*)((char*)workspace + kCutBytes);
+  p.part_o = need > 0 ? (float*)((char*)p.part_ml + ml_bytes(part_rows(cache, args, plan))) : nullptr;
   p.mask = args->mask;
   p.mask_stride = args->mask_stride;
   p.mask_words = (args->T + 63) / 64;
@@ -899,17 +989,13 @@ extern "C" kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcru
   p.T = args->T;
   p.n_split = plan.n_split;
   p.row_tiles = plan.row_tiles;
-  p.groups = cache->B * cache->Hkv * plan.n_split;
+  p.pieces = plan.pieces;
   p.q_dtype = args->dtype;
   p.scale_log2 = (float)(1.4426950408889634 *
                          (args->softmax_scale != 0.0f ? (double)args->softmax_scale : 1.0 / sqrt((double)D)));
   hipStream_t stream = (hipStream_t)hip_stream;
-  st = with_format(cache->format, [&](auto fmt) -> kvcrush_status {
+  return with_format(cache->format, [&](auto fmt) -> kvcrush_status {
     constexpr int FMT = decltype(fmt)::value;
     return D == 128 ? launch_rows<Fmt<FMT, 128>>(p, plan, stream) : launch_rows<Fmt<FMT, 64>>(p, plan, stream);
   });
-  if (st != KVCRUSH_OK || plan.n_split == 1) return st;
-  const dim3 grid((unsigned)plan.rows);
-  return D == 128 ? kvc::launch(attend_merge_kernel<128>, grid, dim3(256), 0, stream, p)
-                  : kvc::launch(attend_merge_kernel<64>, grid, dim3(256), 0, stream, p);
 }

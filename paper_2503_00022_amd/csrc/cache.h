@@ -28,14 +28,15 @@ struct View {
   float* v_param;
   const int32_t* lengths;
   const int32_t* table;  // null: dense
-  int B, Hkv, S, capacity, block_size, n_blocks, table_width;
+  int B, Hkv, S, capacity, block_size, block_shift, n_blocks, table_width;  // block_shift: log2 of a power of two, else -1
 
   __device__ int length(int b) const { return lengths ? min(max(lengths[b], 0), S) : S; }
   // Token `pos` of sequence b as the pool or the sequence counts tokens (a block outside the pool is pulled into it).
   __device__ int token(int b, int pos) const { return table ? paged_token(b, pos) : pos; }
   __device__ int paged_token(int b, int pos) const {
-    const int block = min(max(table[(size_t)b * table_width + pos / block_size], 0), n_blocks - 1);
-    return block * block_size + pos % block_size;
+    const int of = block_shift >= 0 ? pos >> block_shift : pos / block_size;
+    const int block = min(max(table[(size_t)b * table_width + of], 0), n_blocks - 1);
+    return block * block_size + (pos - of * block_size);
   }
   // Row of KV head h = base(b, h) + token * step().
   __device__ size_t base(int b, int h) const { return table ? (size_t)h : ((size_t)b * Hkv + h) * capacity; }
@@ -78,6 +79,7 @@ inline View view(const kvcrush_cache* c) {
   w.S = c->S;
   w.capacity = c->capacity;
   w.block_size = c->block_table ? c->block_size : 1;
+  w.block_shift = (w.block_size & (w.block_size - 1)) == 0 ? __builtin_ctz(w.block_size) : -1;
   w.n_blocks = c->block_table ? c->n_blocks : 1;
   w.table_width = c->block_table ? c->capacity / c->block_size : 0;
   return w;
