@@ -459,6 +459,7 @@ def kvcrush_compact_block_table(idx, block_table, block_size: int, out=None, str
 # ------------------------------------------------------------------------------------------- using the cache
 _FORMATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.float8_e4m3fn: E4M3, torch.int8: I8,
             torch.uint8: I4}
+_VALUES = (torch.float32, torch.bfloat16, torch.float16)
 CODES = {"e4m3": torch.float8_e4m3fn, "i8": torch.int8, "i4": torch.uint8}   # element types of quantised caches
 
 
@@ -495,69 +496,97 @@ def make_cache(k, v, S: int, k_param=None, v_param=None, lengths=None, block_tab
     if any(t is not None and t.device != k.device for t in tensors):
         raise ValueError("the cache's tensors must live on one device")
     cache = Cache(B, Hkv, int(S), D, capacity, fmt, block_size, n_blocks, *(None if t is None else t.data_ptr() for t in tensors))
-    cache.tensors, cache.device, cache.dtype = tensors, k.device, k.dtype
+    cache.tensors, cache.device, cache.index = tensors, k.device, k.get_device()
+    cache.value_dtype = torch.bfloat16 if k.dtype in CODES.values() else k.dtype
+    cache.per_sequence = (B,)
     return cache
 
 
-class _On:
-    """The device of a call's tensors as the current one, and the stream of the call: where tensors made for it are in use."""
-
-    def __init__(self, device, stream):
-        self.index = device.index
-        self.back = torch.cuda.current_device()
-        self.stream = stream
-
-    def __enter__(self):
-        if self.index != self.back:
-            torch.cuda.set_device(self.index)
-        return _stream(self.stream)
-
-    def __exit__(self, *_):
-        if self.index != self.back:
-            torch.cuda.set_device(self.back)
-
-    def used(self, *made):
-        """Tensors made for this call under the current stream that another one uses."""
-        if self.stream is not None:
-            for t in made:
-                t.record_stream(self.stream)
+def _here(t, name: str, index: int):
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on the cache's device" if t.is_cuda else f"{name} must live in GPU memory")
 
 
-def _same_device(cache, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != cache.device:
-            raise ValueError(f"{name} must live on the cache's device")
+def _packed(t, name: str, index: int, dtype, shape):
+    """A contiguous tensor on the cache's device, of this type and shape."""
+    _here(t, name, index)
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {list(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(t, name: str, index: int):
+    """[B,H,T,D] on the cache's device with the D values contiguous (any other strides)."""
+    _here(t, name, index)
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{name} must be [B,H,T,D] with the D values contiguous")
 
 
 def _strides(t):
-    """Element strides of [B,H,T,D] (sequence, head, token); an axis of one element has any, so its packed one is given."""
+    """Element strides of [B,H,T,D] (sequence, head, token), None if packed; an axis of one element has any stride, so its
+    packed one is given."""
     if t.is_contiguous():
         return None
     B, H, T, D = t.shape
     st = t.stride()
-    return (ctypes.c_int64 * 3)(st[0] if B > 1 else H * T * D, st[1] if H > 1 else T * D, st[2] if T > 1 else D)
+    return st[0] if B > 1 else H * T * D, st[1] if H > 1 else T * D, st[2] if T > 1 else D
 
 
-def _count(t, cache, name):
-    if t is None:
-        return None
-    if t.dtype != torch.int32 or tuple(_dev(t, name).shape) != (cache.B,):
-        raise ValueError(f"{name} must be int32 [B]")
-    return t.data_ptr()
+def _stride_array(t):
+    st = _strides(t)
+    return None if st is None else (ctypes.c_int64 * 3)(*st)
+
+
+def _counts(n_new, cache):
+    return None if n_new is None else _packed(n_new, "n_new", cache.index, torch.int32, cache.per_sequence)
+
+
+# The small calls' kernels take a few us, about as long as Python takes for a dozen attribute reads and calls: what a call
+# needs is read once, and the current device changes only where it has to.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+class _Device:
+    """The cache's device as the current one, if it is not."""
+
+    def __init__(self, index):
+        self.index, self.back = index, _current_device()
+
+    def __enter__(self):
+        if self.back != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *_):
+        if self.back != self.index:
+            torch.cuda.set_device(self.back)
+
+
+def _stream_of(cache, stream):
+    return _current_raw_stream(cache.index) if stream is None else stream.cuda_stream
+
+
+def _hand_over(stream, *made):
+    """Tensors made under the current stream for a call that uses them on `stream`."""
+    if stream is not None:
+        for t in made:
+            if t is not None:
+                t.record_stream(stream)
 
 
 def kvcrush_cache_write(cache: Cache, k_new, v_new, n_new=None, stream=None):
     """k_new, v_new [B,Hkv,T,D] (any strides, D contiguous) become the last T tokens of their sequences: the cache's
     lengths count them already.  n_new int32 [B]: only the first n_new[b] of sequence b's are real.  Quantised caches
     take float32, bfloat16 and float16, the others their own type."""
-    _dev_rows(k_new, "k_new"), _dev_rows(v_new, "v_new")
-    T = k_new.shape[2]
-    if v_new.shape != k_new.shape or v_new.dtype != k_new.dtype or tuple(k_new.shape) != (cache.B, cache.Hkv, T, cache.D):
+    index, shape = cache.index, k_new.shape
+    _rows(k_new, "k_new", index), _rows(v_new, "v_new", index)
+    if v_new.shape != shape or v_new.dtype != k_new.dtype or shape[0] != cache.B or shape[1] != cache.Hkv or shape[3] != cache.D:
         raise ValueError("k_new and v_new must be [B,Hkv,T,D] tensors of one type that fit the cache")
-    _same_device(cache, k_new=k_new, v_new=v_new, n_new=n_new)
-    with _On(cache.device, stream) as s:
-        st = load().kvcrush_cache_write(ctypes.byref(cache), T, _dtype_code(k_new), k_new.data_ptr(), v_new.data_ptr(),
-                                        _strides(k_new), _strides(v_new), _count(n_new, cache, "n_new"), s)
+    with _Device(index):
+        st = load().kvcrush_cache_write(cache, shape[2], _dtype_code(k_new), k_new.data_ptr(), v_new.data_ptr(),
+                                        _stride_array(k_new), _stride_array(v_new), _counts(n_new, cache),
+                                        _stream_of(cache, stream))
     _check(st, "kvcrush_cache_write")
 
 
@@ -565,49 +594,47 @@ def kvcrush_cache_read(cache: Cache, idx=None, n=None, dtype=None, k_out=None, v
     """The cache's rows as values: of the positions idx int32 [B,n], or of the first n (default: cache.S) tokens.
     -> (k, v) [B,Hkv,n,D] of `dtype` (default: k_out's; the cache's own type; bfloat16 of quantised ones).  Rows that a
     sequence does not have stay as they are in k_out and v_out; in tensors made here they are zero."""
+    index, at = cache.index, None
     if idx is not None:
-        if idx.dtype != torch.int32 or _dev(idx, "idx").dim() != 2 or idx.shape[0] != cache.B:
-            raise ValueError("idx must be int32 [B,n]")
-        n = idx.shape[1]
+        n = idx.shape[-1]
+        at = _packed(idx, "idx", index, torch.int32, (cache.B, n))
     elif n is None:
         n = cache.S
-    shape = (cache.B, cache.Hkv, int(n), cache.D)
+    shape = (cache.B, cache.Hkv, n, cache.D)
     if dtype is None:
-        dtype = k_out.dtype if k_out is not None else cache.dtype if cache.dtype not in CODES.values() else torch.bfloat16
-    on, made = _On(cache.device, stream), []
-    with on as s:
-        if k_out is None or v_out is None:
-            new = torch.zeros if cache.lengths or idx is None and n > cache.S else torch.empty
-            made = [new(shape, dtype=dtype, device=cache.device) for t in (k_out, v_out) if t is None]
-            if stream is not None and new is torch.zeros:   # (the zeros are written under the current stream)
-                stream.wait_stream(torch.cuda.current_stream())
-            k_out, v_out = (made[0] if k_out is None else k_out), (made[-1] if v_out is None else v_out)
-        for name, t in (("k_out", k_out), ("v_out", v_out)):
-            if tuple(_dev(t, name).shape) != shape or t.dtype != dtype:
-                raise ValueError(f"{name} must be {dtype} {list(shape)}")
-        _same_device(cache, k_out=k_out, v_out=v_out, idx=idx)
-        st = load().kvcrush_cache_read(ctypes.byref(cache), n, _ptr(idx), _dtype_code(k_out), k_out.data_ptr(), v_out.data_ptr(), s)
-        on.used(*made)
+        dtype = k_out.dtype if k_out is not None else v_out.dtype if v_out is not None else cache.value_dtype
+    made_k = made_v = None
+    if k_out is None or v_out is None:
+        # (some rows may stay unwritten: those of sequences shorter than n, of empty ones)
+        new = torch.zeros if cache.lengths or (cache.S < n if idx is None else cache.S == 0) else torch.empty
+        if k_out is None:
+            k_out = made_k = new(shape, dtype=dtype, device=cache.device)
+        if v_out is None:
+            v_out = made_v = new(shape, dtype=dtype, device=cache.device)
+        if stream is not None and new is torch.zeros:   # (the zeros are written under the current stream)
+            stream.wait_stream(torch.cuda.current_stream(cache.device))
+    k_at, v_at = _packed(k_out, "k_out", index, dtype, shape), _packed(v_out, "v_out", index, dtype, shape)
+    with _Device(index):
+        st = load().kvcrush_cache_read(cache, n, at, _dtype_code(k_out), k_at, v_at, _stream_of(cache, stream))
+    _hand_over(stream, made_k, made_v)
     _check(st, "kvcrush_cache_read")
     return k_out, v_out
-
-
-def _attend_sizes(cache, Hq, T, dtype, scale=0.0, n_list=0, unit=0):
-    return AttendArgs(Hq, T, _FORMATS[dtype], float(scale), blocks=16 if n_list else None, n_list=n_list, unit=unit)
 
 
 def kvcrush_attend_workspace(cache: Cache, Hq: int, T: int, dtype, n_list=0, unit=0) -> int:
     """Bytes of scratch memory that kvcrush_attend needs for queries [B,Hq,T,D] of `dtype` (with lists: of n_list blocks
     of `unit` tokens) on this cache, its S and capacity being what they are now; a larger S needs no less."""
-    return int(load().kvcrush_attend_workspace(ctypes.byref(cache), ctypes.byref(_attend_sizes(cache, Hq, T, dtype, 0.0, n_list, unit))))
+    args = AttendArgs(Hq, T, _FORMATS[dtype], blocks=16 if n_list else None, n_list=n_list, unit=unit)
+    return int(load().kvcrush_attend_workspace(cache, args))
 
 
 def _queries(cache, q):
-    _dev_rows(q, "q")
+    _rows(q, "q", cache.index)
     B, Hq, T, D = q.shape
-    if B != cache.B or D != cache.D or q.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+    dtype = q.dtype
+    if B != cache.B or D != cache.D or dtype not in _VALUES:
         raise ValueError("q must be a float32, bfloat16 or float16 [B,Hq,T,D] that fits the cache")
-    args = AttendArgs(Hq, T, _FORMATS[q.dtype])
+    args = AttendArgs(Hq, T, _FORMATS[dtype])
     st = _strides(q)
     if st is not None:
         args.q_stride = st
@@ -622,79 +649,77 @@ def kvcrush_attend(cache: Cache, q, mask=None, n_new=None, blocks=None, unit=0, 
     token t see new token j; without it, those up to itself.  All tokens before the new ones are seen.
     n_new int32 [B]: only the first n_new[b] of the T tokens are real.
     blocks int32 [B,Hkv,T,n] (kvcrush_block_select): query t sees only these blocks of `unit` tokens."""
-    args = _queries(cache, q)
-    B, Hq, T, D = q.shape
-    args.softmax_scale = float(scale)
+    args, index, shape = _queries(cache, q), cache.index, q.shape
+    B, Hq, T, _ = shape
+    args.softmax_scale = scale
     if mask is not None:
         words = (T + 63) // 64
-        if mask.dtype != torch.int64 or tuple(_dev(mask, "mask").shape) not in ((B, T, words), (T, words)):
-            raise ValueError("mask must be int64 [B,T,ceil(T/64)] or [T,ceil(T/64)]")
-        args.mask, args.mask_stride = mask.data_ptr(), T * words if mask.dim() == 3 else 0
+        args.mask = _packed(mask, "mask", index, torch.int64, (B, T, words) if mask.dim() == 3 else (T, words))
+        args.mask_stride = T * words if mask.dim() == 3 else 0
     if blocks is not None:
-        if blocks.dtype != torch.int32 or _dev(blocks, "blocks").dim() != 4 or tuple(blocks.shape[:3]) != (B, cache.Hkv, T):
-            raise ValueError("blocks must be int32 [B,Hkv,T,n]")
-        args.blocks, args.n_list, args.unit = blocks.data_ptr(), blocks.shape[3], int(unit)
-    args.n_new = _count(n_new, cache, "n_new")
-    _same_device(cache, q=q, mask=mask, n_new=n_new, blocks=blocks, out=out, lse=lse, workspace=workspace)
-    L, on, made = load(), _On(cache.device, stream), []
-    with on as s:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=cache.device)
-            made.append(out)
-        else:
-            if tuple(_dev_rows(out, "out").shape) != tuple(q.shape) or out.dtype != q.dtype:
-                raise ValueError("out must have q's shape and type")
-            st = _strides(out)
-            if st is not None:
-                args.out_stride = st
-        if lse is None:
-            lse = torch.empty(B, Hq, T, dtype=torch.float32, device=cache.device)
-            made.append(lse)
-        elif lse.dtype != torch.float32 or tuple(_dev(lse, "lse").shape) != (B, Hq, T):
-            raise ValueError("lse must be float32 [B,Hq,T]")
-        if workspace is None:
-            workspace = torch.empty(max(int(L.kvcrush_attend_workspace(ctypes.byref(cache), ctypes.byref(args))), 16),
-                                    dtype=torch.uint8, device=cache.device)
-            made.append(workspace)
-        st = L.kvcrush_attend(ctypes.byref(cache), ctypes.byref(args), q.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), s)
-        on.used(*made)
+        args.blocks = _packed(blocks, "blocks", index, torch.int32, (B, cache.Hkv, T, blocks.shape[-1]))
+        args.n_list, args.unit = blocks.shape[-1], unit
+    if n_new is not None:
+        args.n_new = _counts(n_new, cache)
+    made_out = made_lse = made_ws = None
+    if out is None:
+        out = made_out = torch.empty(shape, dtype=q.dtype, device=cache.device)
+    else:
+        _rows(out, "out", index)
+        if out.shape != shape or out.dtype != q.dtype:
+            raise ValueError("out must have q's shape and type")
+        st = _strides(out)
+        if st is not None:
+            args.out_stride = st
+    if lse is None:
+        lse = made_lse = torch.empty(shape[:3], dtype=torch.float32, device=cache.device)
+    else:
+        _packed(lse, "lse", index, torch.float32, shape[:3])
+    L = load()
+    if workspace is None:
+        workspace = made_ws = torch.empty(max(L.kvcrush_attend_workspace(cache, args), 16), dtype=torch.uint8, device=cache.device)
+    else:
+        _here(workspace, "workspace", index)
+    with _Device(index):
+        st = L.kvcrush_attend(cache, args, q.data_ptr(), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                              _stream_of(cache, stream))
+    _hand_over(stream, made_out, made_lse, made_ws)
     _check(st, "kvcrush_attend")
     return out, lse
+
+
+def _block_shapes(cache, unit):
+    if unit < 1:
+        raise ValueError("unit must be positive")
+    nb = (cache.capacity + unit - 1) // unit
+    return (cache.B, cache.Hkv, nb, 2, cache.D), (cache.B, cache.Hkv, nb)
 
 
 def kvcrush_block_bounds(cache: Cache, unit: int, bounds=None, scales=None, T=0, n_new=None, stream=None):
     """8-bit bounds of the keys of every block of `unit` tokens: (bounds int8 [B,Hkv,Nb,2,D], scales float32 [B,Hkv,Nb]),
     Nb = ceil(capacity / unit).  T > 0 refreshes, in bounds and scales given, the blocks of the last T tokens (of the
     n_new[b] real ones) only."""
-    if unit < 1:
-        raise ValueError("unit must be positive")
-    nb = (cache.capacity + unit - 1) // unit
+    index = cache.index
+    of_bounds, of_scales = _block_shapes(cache, unit)
     if (bounds is None) != (scales is None) or (bounds is None and T):
         raise ValueError("bounds and scales come together, and are needed to refresh blocks of them")
-    _same_device(cache, bounds=bounds, scales=scales, n_new=n_new)
-    on, made = _On(cache.device, stream), []
-    with on as s:
-        if bounds is None:
-            made = [torch.zeros(cache.B, cache.Hkv, nb, 2, cache.D, dtype=torch.int8, device=cache.device),
-                    torch.zeros(cache.B, cache.Hkv, nb, dtype=torch.float32, device=cache.device)]
-            bounds, scales = made
-            if stream is not None:
-                stream.wait_stream(torch.cuda.current_stream())
-        if bounds.dtype != torch.int8 or tuple(_dev(bounds, "bounds").shape) != (cache.B, cache.Hkv, nb, 2, cache.D):
-            raise ValueError("bounds must be int8 [B,Hkv,ceil(capacity/unit),2,D]")
-        if scales.dtype != torch.float32 or tuple(_dev(scales, "scales").shape) != (cache.B, cache.Hkv, nb):
-            raise ValueError("scales must be float32 [B,Hkv,ceil(capacity/unit)]")
-        st = load().kvcrush_block_bounds(ctypes.byref(cache), unit, T, _count(n_new, cache, "n_new"), bounds.data_ptr(),
-                                         scales.data_ptr(), s)
-        on.used(*made)
+    made = (None, None)
+    if bounds is None:
+        made = bounds, scales = (torch.zeros(of_bounds, dtype=torch.int8, device=cache.device),
+                                 torch.zeros(of_scales, dtype=torch.float32, device=cache.device))
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream(cache.device))
+    bounds_at = _packed(bounds, "bounds", index, torch.int8, of_bounds)
+    scales_at = _packed(scales, "scales", index, torch.float32, of_scales)
+    with _Device(index):
+        st = load().kvcrush_block_bounds(cache, unit, T, _counts(n_new, cache), bounds_at, scales_at, _stream_of(cache, stream))
+    _hand_over(stream, *made)
     _check(st, "kvcrush_block_bounds")
     return bounds, scales
 
 
 def kvcrush_block_select_workspace(cache: Cache, Hq: int, T: int, dtype, unit: int, n_select: int) -> int:
-    return int(load().kvcrush_block_select_workspace(ctypes.byref(cache), ctypes.byref(_attend_sizes(cache, Hq, T, dtype)), unit,
-                                                     n_select))
+    return int(load().kvcrush_block_select_workspace(cache, AttendArgs(Hq, T, _FORMATS[dtype]), unit, n_select))
 
 
 def kvcrush_block_select(cache: Cache, q, bounds, scales, unit: int, n_select: int, n_sink=1, n_recent=1, n_new=None, blocks=None,
@@ -702,30 +727,27 @@ def kvcrush_block_select(cache: Cache, q, bounds, scales, unit: int, n_select: i
     """For each query of q [B,Hq,T,D] and each KV head the n_select blocks to attend to: int32 [B,Hkv,T,n_select],
     ascending, -1 behind the last.  The first n_sink and last n_recent blocks of the sequence are among them, the others
     are those of the largest scores by kvcrush_block_bounds' bounds and scales."""
-    args = _queries(cache, q)
-    B, Hq, T, D = q.shape
-    if unit < 1:
-        raise ValueError("unit must be positive")
-    nb = (cache.capacity + unit - 1) // unit
-    if bounds.dtype != torch.int8 or tuple(_dev(bounds, "bounds").shape) != (B, cache.Hkv, nb, 2, D)             or scales.dtype != torch.float32 or tuple(_dev(scales, "scales").shape) != (B, cache.Hkv, nb):
-        raise ValueError("bounds int8 [B,Hkv,ceil(capacity/unit),2,D] and scales float32 [B,Hkv,ceil(capacity/unit)]")
-    args.n_new = _count(n_new, cache, "n_new")
-    _same_device(cache, q=q, bounds=bounds, scales=scales, n_new=n_new, blocks=blocks, workspace=workspace)
-    L, on, made = load(), _On(cache.device, stream), []
-    with on as s:
-        if blocks is None:
-            blocks = torch.empty(B, cache.Hkv, T, max(int(n_select), 0), dtype=torch.int32, device=cache.device)
-            made.append(blocks)
-        elif blocks.dtype != torch.int32 or tuple(_dev(blocks, "blocks").shape) != (B, cache.Hkv, T, n_select):
-            raise ValueError("blocks must be int32 [B,Hkv,T,n_select]")
-        if workspace is None:
-            need = int(L.kvcrush_block_select_workspace(ctypes.byref(cache), ctypes.byref(args), unit, n_select))
-            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
-            made.append(workspace)
-        st = L.kvcrush_block_select(ctypes.byref(cache), ctypes.byref(args), unit, n_select, n_sink, n_recent, q.data_ptr(),
-                                    bounds.data_ptr(), scales.data_ptr(), blocks.data_ptr(), workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), s)
-        on.used(*made)
+    args, index = _queries(cache, q), cache.index
+    of_bounds, of_scales = _block_shapes(cache, unit)
+    bounds_at = _packed(bounds, "bounds", index, torch.int8, of_bounds)
+    scales_at = _packed(scales, "scales", index, torch.float32, of_scales)
+    if n_new is not None:
+        args.n_new = _counts(n_new, cache)
+    L, made_blocks, made_ws = load(), None, None
+    shape = (cache.B, cache.Hkv, q.shape[2], n_select)
+    if blocks is None:
+        blocks = made_blocks = torch.empty(shape if n_select > 0 else 0, dtype=torch.int32, device=cache.device)
+    else:
+        _packed(blocks, "blocks", index, torch.int32, shape)
+    if workspace is None:
+        need = L.kvcrush_block_select_workspace(cache, args, unit, n_select)
+        workspace = made_ws = torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
+    else:
+        _here(workspace, "workspace", index)
+    with _Device(index):
+        st = L.kvcrush_block_select(cache, args, unit, n_select, n_sink, n_recent, q.data_ptr(), bounds_at, scales_at,
+                                    blocks.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(cache, stream))
+    _hand_over(stream, made_blocks, made_ws)
     _check(st, "kvcrush_block_select")
     return blocks
 

@@ -599,13 +599,8 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
             see = most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
           }
           see = up >= 64 ? 0 : see << up;
-        } else {
-#pragma unroll 1
-          for (int k = 0; k < kTile; ++k) {
-            const int d = __builtin_amdgcn_readlane(draft, k);
-            const bool bit = words ? (words[min(max(d >> 6, 0), last)] >> (d & 63)) & 1 : d <= t_of[c];
-            see |= (uint64_t)bit << k;
-          }
+        } else {  // all rows are heads of one query: each lane asks for its key
+          see = __ballot(words ? (words[min(max(draft >> 6, 0), last)] >> (draft & 63)) & 1 : draft <= t_list);
         }
         see = t_of[c] < n ? (see | old) & there : 0;
 #pragma unroll
@@ -899,20 +894,31 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   const long long keys = a->blocks ? std::min<long long>((long long)a->n_list * a->unit, c->capacity) : c->S;
   // One workgroup to a compute unit: as many pieces as leave the fewest keys to the unit that has most, fewer where that
   // gains nothing.
-  const long long base = (long long)c->Hkv * tiles, most = std::max(1ll, std::min<long long>((keys + 255) / 256, kMaxSplit));
-  if (c->lengths && !a->blocks && c->B > 1 && c->B <= KVC_WAVE && base * c->B < kUnits) {
+  const long long base = (long long)c->Hkv * tiles;
+  int step = 256;  // keys that a workgroup's waves take at a time: no piece is smaller
+  with_format(c->format, [&](auto fmt) {
+    using F128 = Fmt<decltype(fmt)::value, 128>;
+    using F64 = Fmt<decltype(fmt)::value, 64>;
+    step = c->D == 128 ? F128::kTile * F128::waves(plan.NC, plan.RW) / plan.RW : F64::kTile * F64::waves(plan.NC, plan.RW) / plan.RW;
+    return KVCRUSH_OK;
+  });
+  const long long most = std::max(1ll, std::min<long long>((keys + step - 1) / step, kMaxSplit));
+  // Time of n pieces a sequence, in us as measured at both ends: 4 for a workgroup and 1.5 for each tile of its waves, in
+  // rounds of one workgroup to a compute unit; 3.5 to merge pieces.  (2 sequences of 160 keys in one piece, 11.4, or two,
+  // 14.2; 8 of 2048 in four, 18.6, or one, 32.)
+  const long long workgroups = base * c->B, steps = (keys + step - 1) / step;
+  double least = 0.0;
+  plan.n_split = 1;
+  for (long long n = 1; n <= most && n <= 2 * kUnits / workgroups + 1; ++n) {
+    const double us = (double)((workgroups * n + kUnits - 1) / kUnits) * (4.0 + 1.5 * (double)((steps + n - 1) / n)) + (n > 1 ? 3.5 : 0.0);
+    if (n > 1 && us >= 0.97 * least) continue;
+    least = us;
+    plan.n_split = (int)n;
+  }
+  plan.pieces = c->B * plan.n_split;
+  if (plan.n_split > 1 && c->lengths && !a->blocks && c->B > 1 && c->B <= KVC_WAVE) {
     plan.n_split = 0;
     plan.pieces = (int)std::max<long long>(c->B, std::min(kUnits / base, most * c->B));
-  } else {
-    plan.n_split = 1;
-    double least = 0.0;
-    for (int n = 1; n <= most; ++n) {
-      const double keys_of_unit = (double)((base * c->B * n + kUnits - 1) / kUnits) / n;
-      if (n > 1 && keys_of_unit > 0.95 * least) continue;
-      least = keys_of_unit;
-      plan.n_split = n;
-    }
-    plan.pieces = c->B * plan.n_split;
   }
   return KVCRUSH_OK;
 }

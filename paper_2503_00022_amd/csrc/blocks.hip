@@ -191,11 +191,20 @@ __global__ __launch_bounds__(THREADS) void block_choose_kernel(SelectParams p) {
   uint32_t* counts = keys + ((nb + 63) & ~63);
   const float* scores = p.scores + (size_t)row * p.n_stride;
   uint32_t lo = ~0u, hi = 0;
-  for (int i = tid; i < nb; i += THREADS) {
-    const bool forced = i < p.n_sink || i >= nb - p.n_recent;
-    const uint32_t k = forced ? ~0u : min(order_key(scores[i]), ~0u - 1);
-    keys[i] = k;
-    if (!forced) lo = min(lo, k), hi = max(hi, k);
+  constexpr int kAhead = 4;  // loads of a lane under way together
+  for (int i0 = tid; i0 < nb; i0 += kAhead * THREADS) {
+    float x[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x[u] = scores[min(i0 + u * THREADS, nb - 1)];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u * THREADS;
+      if (i >= nb) break;
+      const bool forced = i < p.n_sink || i >= nb - p.n_recent;
+      const uint32_t k = forced ? ~0u : min(order_key(x[u]), ~0u - 1);
+      keys[i] = k;
+      if (!forced) lo = min(lo, k), hi = max(hi, k);
+    }
   }
   lo = kvc::wave_min(lo);
   hi = ~kvc::wave_min(~hi);
@@ -390,7 +399,7 @@ extern "C" kvcrush_status kvcrush_block_select(const kvcrush_cache* cache, const
   }
   const size_t lds = ((size_t)p.n_stride + 2 * (p.n_stride / 64)) * sizeof(uint32_t);
   const dim3 grid((unsigned)((size_t)cache->B * cache->Hkv * args->T));
-  if (nb <= 4096) return kvc::launch(block_choose_kernel<256>, grid, dim3(256), lds, stream, p);
+  if (nb <= 1024) return kvc::launch(block_choose_kernel<256>, grid, dim3(256), lds, stream, p);
   st = kvc::allow_large_lds<block_choose_kernel<1024>>(2048);
   return st != KVCRUSH_OK ? st : kvc::launch(block_choose_kernel<1024>, grid, dim3(1024), lds, stream, p);
 }

@@ -103,14 +103,26 @@ inline bool strides_ok(const int64_t* s, int H, int T, int D, int bytes, int64_t
 // (a function: __builtin_bit_cast of a vector's element takes the vector's first one, whichever is named)
 __device__ __forceinline__ f16x2 as_f16x2(uint32_t w) { return __builtin_bit_cast(f16x2, w); }
 
-template <int DTYPE>
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16(const char* at) {
+  return ONCE ? __builtin_nontemporal_load((const u32x4*)at) : *(const u32x4*)at;
+}
+template <bool ONCE>
+__device__ __forceinline__ void store16(char* at, const u32x4& v) {
+  if (ONCE)
+    __builtin_nontemporal_store(v, (u32x4*)at);
+  else
+    *(u32x4*)at = v;
+}
+
+template <int DTYPE, bool ONCE = false>
 __device__ __forceinline__ void load8(const char* at, float (&x)[8]) {  // eight values, 16 or 32 bytes
   if constexpr (DTYPE == KVCRUSH_F32) {
-    const u32x4 a = *(const u32x4*)at, b = *(const u32x4*)(at + 16);
+    const u32x4 a = load16<ONCE>(at), b = load16<ONCE>(at + 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(a[i]), x[4 + i] = __uint_as_float(b[i]);
   } else {
-    const u32x4 a = *(const u32x4*)at;
+    const u32x4 a = load16<ONCE>(at);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (DTYPE == KVCRUSH_BF16) {
@@ -137,13 +149,13 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   }
 }
 
-template <int DTYPE>
+template <int DTYPE, bool ONCE = false>
 __device__ __forceinline__ void store8(char* at, const float (&x)[8]) {
   if constexpr (DTYPE == KVCRUSH_F32) {
-    *(u32x4*)at = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
-    *(u32x4*)(at + 16) = u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
+    store16<ONCE>(at, u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])});
+    store16<ONCE>(at + 16, u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])});
   } else {
-    *(u32x4*)at = u32x4{pack2<DTYPE>(x[0], x[1]), pack2<DTYPE>(x[2], x[3]), pack2<DTYPE>(x[4], x[5]), pack2<DTYPE>(x[6], x[7])};
+    store16<ONCE>(at, u32x4{pack2<DTYPE>(x[0], x[1]), pack2<DTYPE>(x[2], x[3]), pack2<DTYPE>(x[4], x[5]), pack2<DTYPE>(x[6], x[7])});
   }
 }
 

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(WriteParams p) {
   for (int u = 0; u < ROWS; ++u) {
     const int t = t0 + u * kGroup;
     if (t < n) {
-      load8<DTYPE>(src + (size_t)t * p.stride[which][2] * (format_bits(DTYPE) / 8), x[u]);
+      load8<DTYPE, (ROWS > 1)>(src + (size_t)t * p.stride[which][2] * (format_bits(DTYPE) / 8), x[u]);
       token[u] = p.c.token(b, L - n + t);
     }
   }
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(ReadParams p) {
 #pragma unroll
   for (int u = 0; u < ROWS; ++u) {
     const int j = j0 + u * kGroup;
-    if (j < end) store8<DTYPE>(dst + (size_t)j * D * (format_bits(DTYPE) / 8), x[u]);
+    if (j < end) store8<DTYPE, (ROWS > 1)>(dst + (size_t)j * D * (format_bits(DTYPE) / 8), x[u]);
   }
 }
 

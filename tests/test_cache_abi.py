@@ -150,12 +150,12 @@ def test_binding_refuses_host_memory_and_wrong_shapes():
     with pytest.raises(ValueError, match="GPU memory"):
         kv.make_cache(k, k, 10)
     c = cache()
-    c.tensors, c.device, c.dtype = (), torch.device("cuda", 0), torch.int8
+    c.tensors, c.device, c.index, c.value_dtype, c.per_sequence = (), torch.device("cuda", 0), 0, torch.bfloat16, (2,)
     with pytest.raises(ValueError, match="GPU memory"):
         kv.kvcrush_attend(c, torch.zeros(2, 4, 1, 128))
     with pytest.raises(ValueError, match="GPU memory"):
         kv.kvcrush_cache_write(c, torch.zeros(2, 2, 1, 128), torch.zeros(2, 2, 1, 128))
-    with pytest.raises(ValueError, match="idx"):
+    with pytest.raises(ValueError, match="GPU memory"):
         kv.kvcrush_cache_read(c, idx=torch.zeros(2, 3))
     with pytest.raises(ValueError, match="unit"):
         kv.kvcrush_block_bounds(c, 0)
