@@ -865,6 +865,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
 // ------------------------------------------------------------------------------------ host
 struct Plan {
   int G, NC, RW, row_tiles, n_split, pieces;  // n_split 0: dealt by length
+  int most_pieces;                            // that any length up to this one has
   long long rows;  // B * Hq * T
 };
 
@@ -907,9 +908,10 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   // rounds of one workgroup to a compute unit; 3.5 to merge pieces.  (2 sequences of 160 keys in one piece, 11.4, or two,
   // 14.2; 8 of 2048 in four, 18.6, or one, 32.)
   const long long workgroups = base * c->B, steps = (keys + step - 1) / step;
+  const long long n_end = std::min(most, 2 * kUnits / workgroups + 1);
   double least = 0.0;
   plan.n_split = 1;
-  for (long long n = 1; n <= most && n <= 2 * kUnits / workgroups + 1; ++n) {
+  for (long long n = 1; n <= n_end; ++n) {
     const double us = (double)((workgroups * n + kUnits - 1) / kUnits) * (4.0 + 1.5 * (double)((steps + n - 1) / n)) + (n > 1 ? 3.5 : 0.0);
     if (n > 1 && us >= 0.97 * least) continue;
     least = us;
@@ -918,15 +920,17 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   plan.pieces = c->B * plan.n_split;
   if (plan.n_split > 1 && c->lengths && !a->blocks && c->B > 1 && c->B <= KVC_WAVE) {
     plan.n_split = 0;
-    plan.pieces = (int)std::max<long long>(c->B, std::min(kUnits / base, most * c->B));
+    plan.pieces = (int)std::max<long long>(c->B, std::min(kUnits / base, n_end * c->B));
   }
+  plan.most_pieces = (int)(n_end * c->B);
   return KVCRUSH_OK;
 }
 
 constexpr size_t kCutBytes = KVC_WAVE * sizeof(int2);
-bool merged(const Plan& p) { return p.n_split != 1; }
+// The scratch memory is that of the most pieces, so that a longer sequence never needs less than a shorter one.
+bool merged(const Plan& p) { return p.most_pieces > p.pieces || p.n_split != 1; }
 long long part_rows(const kvcrush_cache* c, const kvcrush_attend_args* a, const Plan& p) {
-  return (long long)a->Hq * a->T * p.pieces;
+  return (long long)a->Hq * a->T * p.most_pieces;
 }
 size_t ml_bytes(long long rows) { return kvc::align_up((size_t)rows * sizeof(float2), 256); }
 size_t plan_bytes(const kvcrush_cache* c, const kvcrush_attend_args* a, const Plan& p) {

@@ -1,5 +1,6 @@
-"""Call sequences over the C ABI for the two ways the library is used: compressing a
-layer's cache after prefill, and keeping a compressed cache while decoding.
+"""Call sequences over the C ABI for the ways the library is used: compressing a layer's
+cache after prefill, keeping a compressed cache while decoding, and generating with a cache
+that is paged, quantised or attended to in parts.
 
 Nothing here computes: the classes own the buffers (outputs, workspaces, the
 ping-pong halves of a decoding cache), pass device pointers to the library and
@@ -109,6 +110,7 @@ class DecodeCache:
             B, Hs, capacity, budget, n_important, bit_topk, anchor, anchor_seed, None, n_sink, n_recent, capacity)), 16),
             dtype=torch.uint8, device=dev)
         self._idx = torch.empty(B, budget, dtype=torch.int32, device=dev)
+        self._views, self._attend_ws = [None, None], None    # made by the first attend
         self.evictions = 0
 
     k = property(lambda self: self._sets[self._cur][0])
@@ -164,3 +166,120 @@ class DecodeCache:
                                      scale=self.scale)
         self.n, self._append_ws = n, workspace  # (a refused call leaves the cache as long as it was, and no workspace)
         return n
+
+    def attend(self, q_new):
+        """The newest token attends to the whole cache, itself included: q_new [B,Hq,D] as append was given ->
+        (out like q_new, lse float32 [B,Hq]).  Tensors on the device are used where they are; nothing is kept of them."""
+        if q_new.dim() != 3:
+            raise ValueError("q_new must be [B,Hq,D]")
+        view = self._views[self._cur]
+        if view is None:
+            view = self._views[self._cur] = kv.make_cache(self.k, self.v, self.n)
+        q = q_new.unsqueeze(2)
+        if self._attend_ws is None or self._attend_ws[0] != q_new.shape[1]:
+            view.S = self.capacity
+            need = kv.kvcrush_attend_workspace(view, q_new.shape[1], 1, q_new.dtype)
+            self._attend_ws = q_new.shape[1], torch.empty(max(need, 16), dtype=torch.uint8, device=self.k.device)
+        view.S = self.n
+        out, lse = kv.kvcrush_attend(view, q, scale=self.scale, workspace=self._attend_ws[1])
+        return out.squeeze(2), lse.squeeze(2)
+
+
+class KVCache:
+    """A layer's KV cache that a model generates with: written as tokens come, attended to by one new token, a chain or a
+    tree of drafted ones, over all of it or over the blocks that suit each query.
+
+    B sequences of up to `capacity` tokens.  `format`: None keeps rows in `dtype`; "e4m3", "i8" and "i4" quantise them as
+    they are written.  `block_size` > 0: paged, with `block_table` int32 [B, capacity / block_size] into a pool of
+    `n_blocks` (without one, sequence b owns blocks b * capacity / block_size and following).  `unit` > 0 keeps bounds of
+    blocks of that many tokens, which attend(n_select=..) chooses by.
+    lengths (int32 [B] on the GPU) counts each sequence's tokens; nothing here synchronises.  The calls capture into a HIP
+    graph once each has run outside one (workspaces are made then); a graph keeps the bound on the lengths of its capture,
+    so capture with `bound` set to what the replays will need."""
+
+    def __init__(self, B, Hkv, capacity, D, dtype=torch.bfloat16, *, format=None, block_size=0, block_table=None, n_blocks=0,
+                 unit=0, scale=0.0, device="cuda"):
+        if format is not None and format not in kv.CODES:
+            raise ValueError(f"format must be None or one of {sorted(kv.CODES)}")
+        if block_size and capacity % block_size:
+            raise ValueError("capacity must be a multiple of block_size")
+        if block_table is not None and not block_size:
+            raise ValueError("a block_table needs a block_size")
+        dev = torch.device(device)
+        if block_size:
+            per = capacity // block_size
+            if block_table is None:
+                block_table = torch.arange(B * per, dtype=torch.int32, device=dev).view(B, per)
+                n_blocks = max(n_blocks, B * per)
+            rows = (n_blocks, block_size, Hkv)
+        else:
+            rows = (B, Hkv, capacity)
+        stored, width = (dtype, D) if format is None else (kv.CODES[format], D // 2 if format == "i4" else D)
+        new = lambda *shape, dtype: torch.zeros(*shape, dtype=dtype, device=dev)  # noqa: E731
+        self.k, self.v = (new(*rows, width, dtype=stored) for _ in range(2))
+        self.k_param = self.v_param = None
+        if format is not None:
+            self.k_param, self.v_param = (new(*rows, *((2,) if format == "i4" else ()), dtype=torch.float32) for _ in range(2))
+        self.lengths, self.block_table = new(B, dtype=torch.int32), block_table
+        self.capacity, self.dtype, self.unit, self.scale, self.bound = capacity, dtype, unit, scale, 0
+        self.cache = kv.make_cache(self.k, self.v, 0, self.k_param, self.v_param, self.lengths, block_table)
+        self.bounds = self.bound_scales = None
+        if unit:
+            nb = (capacity + unit - 1) // unit
+            self.bounds, self.bound_scales = new(B, Hkv, nb, 2, D, dtype=torch.int8), new(B, Hkv, nb, dtype=torch.float32)
+        self._ws = {}
+
+    def append(self, k_new, v_new, n_new=None):
+        """k_new, v_new [B,Hkv,T,D]: T tokens more for every sequence, or the first n_new[b] (int32 [B] on the GPU) of them.
+        A sequence must not outgrow the capacity (the caller's to see to where n_new decides)."""
+        T = k_new.shape[2]
+        if n_new is None and self.bound + T > self.capacity:
+            raise ValueError(f"{T} tokens more may pass the capacity of {self.capacity}: set `bound` to the longest length")
+        before = self.bound, self.cache.S
+        self.bound = self.cache.S = min(self.bound + T, self.capacity)
+        self.lengths.add_(T if n_new is None else n_new)
+        try:
+            kv.kvcrush_cache_write(self.cache, k_new, v_new, n_new=n_new)
+            if self.unit:
+                kv.kvcrush_block_bounds(self.cache, self.unit, self.bounds, self.bound_scales, T=T, n_new=n_new)
+        except Exception:   # (a refused call leaves the cache as long as it was)
+            self.lengths.sub_(T if n_new is None else n_new)
+            self.bound, self.cache.S = before
+            raise
+
+    def drop(self, n):
+        """The last n tokens (a number, or int32 [B] on the GPU) of every sequence are taken back, as rejected drafts are."""
+        self.lengths.sub_(n)
+        if isinstance(n, int):
+            self.bound = self.cache.S = max(self.bound - n, 0)
+
+    def attend(self, q, mask=None, n_new=None, n_select=0, n_sink=1, n_recent=1):
+        """The last T tokens attend to the cache: q [B,Hq,T,D], mask and n_new as kvcrush_attend takes them -> (out, lse).
+        n_select > 0: each query attends only to that many blocks of `unit` tokens, the first n_sink and last n_recent of
+        its sequence among them."""
+        if n_select and not self.unit:
+            raise ValueError("n_select needs a cache with a unit")
+        B, Hq, T, D = q.shape
+        blocks, cache = None, self.cache
+        if n_select:
+            key = "select", Hq, T, q.dtype, n_select
+            ws = self._workspace(key, lambda: kv.kvcrush_block_select_workspace(cache, Hq, T, q.dtype, self.unit, n_select))
+            blocks = kv.kvcrush_block_select(cache, q, self.bounds, self.bound_scales, self.unit, n_select, n_sink, n_recent,
+                                             n_new=n_new, workspace=ws)
+        ws = self._workspace(("attend", Hq, T, q.dtype, n_select),
+                             lambda: kv.kvcrush_attend_workspace(cache, Hq, T, q.dtype, n_list=n_select, unit=self.unit))
+        return kv.kvcrush_attend(cache, q, mask=mask, n_new=n_new, blocks=blocks, unit=self.unit, scale=self.scale, workspace=ws)
+
+    def _workspace(self, key, size):
+        ws = self._ws.get(key)
+        if ws is None:   # (large enough for any length: of the sizes for all lengths, that of the capacity is the largest)
+            now, self.cache.S = self.cache.S, self.capacity
+            try:
+                ws = self._ws[key] = torch.empty(max(size(), 16), dtype=torch.uint8, device=self.lengths.device)
+            finally:
+                self.cache.S = now
+        return ws
+
+    def read(self, idx=None, n=None, dtype=None):
+        """Rows as values: of positions idx int32 [B,n], or the first n (default: the bound on the lengths) -> (k, v)."""
+        return kv.kvcrush_cache_read(self.cache, idx=idx, n=n, dtype=dtype or self.dtype)

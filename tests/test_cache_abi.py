@@ -123,6 +123,17 @@ def test_attend_refusals(lib):
     assert sizes == sorted(sizes)                                                 # a growing cache needs no less
 
 
+@pytest.mark.parametrize("B,Hkv,Hq,T,D,fmt,lengths", [
+    (1, 8, 32, 1, 128, kv.BF16, None), (3, 5, 10, 1, 64, kv.I4, FAKE), (1, 1, 4, 40, 128, kv.I8, None), (7, 8, 8, 3, 128, kv.E4M3, FAKE),
+    (40, 4, 8, 1, 64, kv.F16, FAKE), (2, 2, 64, 5, 128, kv.F32, None)])
+def test_a_growing_cache_never_needs_less_scratch_memory(lib, B, Hkv, Hq, T, D, fmt, lengths):
+    """A workspace sized for the capacity serves every length on the way there."""
+    args = attend_args(Hq=Hq, T=T, dtype=kv.BF16 if fmt > 2 else fmt)
+    sizes = [lib.kvcrush_attend_workspace(ctypes.byref(cache(B=B, Hkv=Hkv, D=D, format=fmt, S=s, capacity=40000, lengths=lengths)),
+                                          ctypes.byref(args)) for s in [*range(0, 6000, 7), *range(6000, 40000, 331)]]
+    assert sizes == sorted(sizes) and sizes[-1] > 0
+
+
 def test_block_refusals(lib):
     def bounds(c=None, unit=16, T=0, b=FAKE, s=FAKE):
         return lib.kvcrush_block_bounds(ctypes.byref(c or cache()), unit, T, None, b, s, None)
