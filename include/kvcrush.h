@@ -380,7 +380,8 @@ typedef enum {
  *              parameters s = d / 15 and lo; the values are lo + s * code (one rounding).
  *              d < 2^-100: s = 0 and codes 0.
  * A row with a value (or a difference d) that is not finite gets NaN as its parameters: it
- * reads back as NaN throughout.
+ * reads back as NaN throughout.  (A row that reaches fp32's largest value may read back as
+ * infinity there: the rounded s times Q.)
  */
 typedef struct {
   int32_t B;           /* sequences                                                              */
@@ -388,7 +389,7 @@ typedef struct {
   int32_t S;           /* valid tokens of every sequence, 0 <= S <= capacity; with lengths: their */
                        /* upper bound                                                            */
   int32_t D;           /* values per row: 64 or 128                                              */
-  int32_t capacity;    /* tokens a sequence has room for                                         */
+  int32_t capacity;    /* tokens a sequence has room for, at most 2^29                           */
   int32_t format;      /* kvcrush_dtype or kvcrush_format                                        */
   int32_t block_size;  /* paged caches only: tokens per block; capacity % block_size == 0        */
   int32_t n_blocks;    /* paged caches only: blocks of the pool, n_blocks * block_size < 2^31    */
@@ -413,7 +414,7 @@ typedef struct {
  *   dtype   of k_new and v_new (kvcrush_dtype); a cache that is not quantised takes its own type only
  *   k_new, v_new  [B, Hkv, T, D], the D values contiguous; k_stride, v_stride (host): NULL (packed),
  *           or elements between consecutive sequences, heads and tokens, multiples of 16 bytes
- * Size limits here and in kvcrush_cache_read: B <= 32767, Hkv <= 65535. */
+ * Size limits here and in kvcrush_cache_read: B <= 32767, Hkv <= 65535, n <= 2^29. */
 kvcrush_status kvcrush_cache_write(const kvcrush_cache* cache, int32_t T, int32_t dtype, const void* k_new,
                                    const void* v_new, const int64_t* k_stride, const int64_t* v_stride,
                                    const int32_t* n_new, void* hip_stream);
@@ -456,8 +457,10 @@ typedef struct {
   int32_t unit;          /* tokens per listed block, 1 <= unit (blocks only)                        */
 } kvcrush_attend_args;
 
-/* Size limits: B * Hkv <= 65535, n_list * unit < 2^30.  lse may be NULL.  The order of summation depends on
- * the arguments' sizes only: equal calls give equal bits. */
+/* Size limits: B * Hkv <= 65535, B * Hq * T <= 2^22, n_list * unit < 2^30.  lse may be NULL.  The order of
+ * summation depends on the arguments' sizes and the lengths only: equal calls give equal bits.
+ * A cache with a larger S never needs a smaller workspace than one with a smaller S: one sized for S = capacity
+ * serves a growing cache. */
 size_t kvcrush_attend_workspace(const kvcrush_cache* cache, const kvcrush_attend_args* args);
 kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcrush_attend_args* args, const void* q, void* out,
                               float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -482,7 +485,8 @@ kvcrush_status kvcrush_block_bounds(const kvcrush_cache* cache, int32_t unit, in
  *   bounds, scales  as kvcrush_block_bounds leaves them
  *   blocks  [B, Hkv, T, n_select] int32: ascending; -1 where the sequence has no more blocks, and for padding
  * Of args only Hq, T, dtype, q_stride and n_new are read (dtype may be any of q's types on any cache).
- * Size limits: ceil(S / unit) <= 32768, Hq / Hkv <= 1024, B * Hkv <= 65535; 0 <= n_sink + n_recent <= n_select. */
+ * Size limits: ceil(S / unit) <= 32768, Hq / Hkv <= 1024, B * Hkv <= 65535, B * Hkv * T <= 2^21;
+ * 0 <= n_sink + n_recent <= n_select. */
 size_t kvcrush_block_select_workspace(const kvcrush_cache* cache, const kvcrush_attend_args* args, int32_t unit,
                                       int32_t n_select);
 kvcrush_status kvcrush_block_select(const kvcrush_cache* cache, const kvcrush_attend_args* args, int32_t unit,

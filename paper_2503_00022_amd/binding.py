@@ -495,6 +495,8 @@ def make_cache(k, v, S: int, k_param=None, v_param=None, lengths=None, block_tab
     tensors = (k, v, k_param, v_param, lengths, block_table)
     if any(t is not None and t.device != k.device for t in tensors):
         raise ValueError("the cache's tensors must live on one device")
+    if any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("the cache's tensors must not require gradients: the calls on it have none")
     cache = Cache(B, Hkv, int(S), D, capacity, fmt, block_size, n_blocks, *(None if t is None else t.data_ptr() for t in tensors))
     cache.tensors, cache.device, cache.index = tensors, k.device, k.get_device()
     cache.value_dtype = torch.bfloat16 if k.dtype in CODES.values() else k.dtype
@@ -522,6 +524,8 @@ def _rows(t, name: str, index: int):
     _here(t, name, index)
     if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
         raise ValueError(f"{name} must be [B,H,T,D] with the D values contiguous")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and the calls on a cache have none: use torch.no_grad() or detach()")
 
 
 def _strides(t):

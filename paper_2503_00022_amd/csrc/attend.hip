@@ -901,7 +901,7 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   if (!(a->softmax_scale >= 0.0f) || a->softmax_scale > 1.0e6f) return KVCRUSH_ERR_INVALID_ARG;
   if (a->mask_stride < 0) return KVCRUSH_ERR_INVALID_ARG;
   if (a->blocks && (a->n_list < 1 || a->unit < 1)) return KVCRUSH_ERR_INVALID_ARG;
-  if (a->T > 1024 || (long long)c->B * a->Hq * a->T > (1 << 24) || (long long)c->B * c->Hkv > 65535 || c->capacity > (1 << 30)) return KVCRUSH_ERR_UNSUPPORTED;
+  if (a->T > 1024 || (long long)c->B * a->Hq * a->T > (1 << 22) || (long long)c->B * c->Hkv > 65535) return KVCRUSH_ERR_UNSUPPORTED;
   if (a->blocks && (long long)a->n_list * a->unit >= (1 << 30)) return KVCRUSH_ERR_UNSUPPORTED;
   plan.G = a->Hq / c->Hkv;
   plan.rows = (long long)c->B * a->Hq * a->T;

@@ -310,7 +310,8 @@ kvcrush_status select_ok(const kvcrush_cache* c, const kvcrush_attend_args* a, i
   if (st != KVCRUSH_OK) return st;
   if (!a || a->Hq < 1 || a->Hq % c->Hkv != 0 || a->T < 1 || !is_dtype(a->dtype) || unit < 1 || n_select < 1)
     return KVCRUSH_ERR_INVALID_ARG;
-  if (a->T > 1024 || a->Hq / c->Hkv > 1024 || (long long)c->B * c->Hkv > 65535) return KVCRUSH_ERR_UNSUPPORTED;
+  if (a->T > 1024 || a->Hq / c->Hkv > 1024 || (long long)c->B * c->Hkv > 65535 || (long long)c->B * c->Hkv * a->T > (1 << 21))
+    return KVCRUSH_ERR_UNSUPPORTED;
   if (((long long)c->S + unit - 1) / unit > kMaxBlocks) return KVCRUSH_ERR_UNSUPPORTED;
   return KVCRUSH_OK;
 }

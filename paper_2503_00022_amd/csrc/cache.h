@@ -12,6 +12,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+constexpr int kMostTokens = 1 << 29;  // of a sequence: grids stay below 2^32 threads
 constexpr float kTiny = 0x1p-100f;  // rows (ranges) below this are stored as zero: 448 / a stays finite above it
 
 __host__ __device__ constexpr int format_bits(int format) {
@@ -62,7 +63,7 @@ inline kvcrush_status check(const kvcrush_cache* c) {
     if (c->block_size < 1 || c->n_blocks < 1 || c->capacity % c->block_size != 0) return KVCRUSH_ERR_INVALID_ARG;
     if ((long long)c->n_blocks * c->block_size > 0x7FFFFFFFll) return KVCRUSH_ERR_UNSUPPORTED;
   }
-  if (c->D != 64 && c->D != 128) return KVCRUSH_ERR_UNSUPPORTED;
+  if ((c->D != 64 && c->D != 128) || c->capacity > kMostTokens) return KVCRUSH_ERR_UNSUPPORTED;
   return KVCRUSH_OK;
 }
 

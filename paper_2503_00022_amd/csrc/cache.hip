@@ -173,7 +173,7 @@ extern "C" kvcrush_status kvcrush_cache_write(const kvcrush_cache* cache, int32_
   if (st != KVCRUSH_OK) return st;
   if (T < 0 || !is_dtype(dtype)) return KVCRUSH_ERR_INVALID_ARG;
   if (!quantised(cache->format) && dtype != cache->format) return KVCRUSH_ERR_INVALID_ARG;
-  if (T == 0) return KVCRUSH_OK;
+  if (T == 0 || cache->S == 0) return KVCRUSH_OK;  // (no token is new)
   if (!k_new || !v_new || !kvc::aligned16(k_new) || !kvc::aligned16(v_new)) return KVCRUSH_ERR_INVALID_ARG;
   WriteParams p;
   p.c = view(cache);
@@ -186,8 +186,9 @@ extern "C" kvcrush_status kvcrush_cache_write(const kvcrush_cache* cache, int32_
   p.T = T;
   const int group = kThreads / (cache->D / 8);
   dim3 grid;
-  const bool few = T <= group;
-  if (!grid_for(cache, group * (few ? 1 : kRows), T, grid)) return KVCRUSH_ERR_UNSUPPORTED;
+  const int most = std::min(T, cache->S);  // (no sequence has more new tokens)
+  const bool few = most <= group;
+  if (!grid_for(cache, group * (few ? 1 : kRows), most, grid)) return KVCRUSH_ERR_UNSUPPORTED;
   return with_dtype(dtype, [&](auto dt) {
     return with_format(cache->format, [&](auto fmt) -> kvcrush_status {
       constexpr int DT = decltype(dt)::value, FMT = decltype(fmt)::value;
@@ -212,6 +213,7 @@ extern "C" kvcrush_status kvcrush_cache_read(const kvcrush_cache* cache, int32_t
   if (n < 0 || (!idx && n > cache->capacity) || !is_dtype(dtype)) return KVCRUSH_ERR_INVALID_ARG;
   if (!quantised(cache->format) && dtype != cache->format) return KVCRUSH_ERR_INVALID_ARG;
   if (n == 0) return KVCRUSH_OK;
+  if (n > kMostTokens) return KVCRUSH_ERR_UNSUPPORTED;
   if (!k_out || !v_out || !kvc::aligned16(k_out) || !kvc::aligned16(v_out)) return KVCRUSH_ERR_INVALID_ARG;
   ReadParams p;
   p.c = view(cache);

@@ -53,7 +53,7 @@ def attend(lib, c=None, args=None, q=FAKE, out=FAKE, lse=FAKE, ws=FAKE, ws_bytes
 
 BAD_CACHES = [
     (dict(B=0), INVALID), (dict(Hkv=0), INVALID), (dict(S=-1), INVALID), (dict(S=129), INVALID), (dict(capacity=0, S=0), INVALID),
-    (dict(format=6), INVALID), (dict(format=-1), INVALID), (dict(D=0), INVALID), (dict(D=96), UNSUPPORTED), (dict(D=256), UNSUPPORTED),
+    (dict(format=6), INVALID), (dict(format=-1), INVALID), (dict(D=0), INVALID), (dict(D=96), UNSUPPORTED), (dict(D=256), UNSUPPORTED), (dict(capacity=(1 << 29) + 1), UNSUPPORTED),
     (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(k=ODD), INVALID), (dict(v=ODD), INVALID), (dict(k_param=None), INVALID),
     (dict(v_param=None), INVALID), (dict(v_param=ODD), INVALID)]
 BAD_PAGED = [(dict(block_size=0), INVALID), (dict(n_blocks=0), INVALID), (dict(block_size=24), INVALID),
@@ -85,6 +85,8 @@ def test_write_and_read_refusals(lib):
     assert write(lib, T=-1) == INVALID and write(lib, dtype=3) == INVALID
     assert write(lib, k=None) == INVALID and write(lib, v=ODD) == INVALID
     assert write(lib, T=0, k=None, v=None) == OK                                  # nothing to do
+    assert write(lib, S=0, k=None, v=None) == OK
+    assert read(lib, n=(1 << 29) + 1) == UNSUPPORTED
     assert write(lib, ks=strides(512, 128, 130)) == INVALID                       # not a multiple of 16 bytes
     assert write(lib, vs=strides(512, -128, 128)) == INVALID
     assert write(lib, vs=strides(1 << 42, 128, 128)) == INVALID
@@ -99,7 +101,7 @@ def test_write_and_read_refusals(lib):
 
 def test_attend_refusals(lib):
     assert attend(lib, Hq=5) == INVALID and attend(lib, Hq=0) == INVALID and attend(lib, T=0) == INVALID
-    assert attend(lib, T=1025) == UNSUPPORTED
+    assert attend(lib, T=1025) == UNSUPPORTED and attend(lib, cache(B=5000), T=1024) == UNSUPPORTED
     assert attend(lib, dtype=kv.F32) == INVALID                                   # float queries on a quantised cache
     assert attend(lib, cache(format=kv.F16), dtype=kv.BF16) == INVALID
     assert attend(lib, dtype=4) == INVALID
@@ -149,7 +151,7 @@ def test_block_refusals(lib):
     assert select(sink=2 ** 31 - 1, recent=2 ** 31 - 1) == INVALID
     assert select(q=None) == INVALID and select(b=ODD) == INVALID and select(s=None) == INVALID and select(out=ODD) == INVALID
     assert select(Hq=3) == INVALID and select(T=1025) == UNSUPPORTED and select(q_stride=(1, 1, 1)) == INVALID
-    assert select(cache(Hkv=1), Hq=1025) == UNSUPPORTED
+    assert select(cache(Hkv=1), Hq=1025) == UNSUPPORTED and select(cache(B=2000), T=1024) == UNSUPPORTED
     assert select(cache(S=40000, capacity=40000), unit=1) == UNSUPPORTED
     need = lib.kvcrush_block_select_workspace(ctypes.byref(cache()), ctypes.byref(attend_args()), 1, 4)
     assert need >= 2 * 2 * 4 * 100 * 4

@@ -495,3 +495,79 @@ def test_calls_on_another_stream():
         side.synchronize()
         assert torch.equal(blocks, want_b) and torch.equal(bits(got[0]), bits(want[0])) and torch.equal(got[1], want[1])
         assert all(torch.equal(bits(x), bits(y)) for x, y in zip(rows, rows2))
+
+
+def test_gradients_are_refused():
+    """The calls are for inference: a tensor that autograd follows is turned down rather than cut off from its gradient."""
+    c = ref.Case("bf16", 1, 2, [20], 64, seed=3).cuda()
+    cache = c.make(kv)
+    q = values((1, 4, 1, 64), "bf16", 1).cuda().requires_grad_()
+    k = values((1, 2, 1, 64), "bf16", 2).cuda().requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        kv.kvcrush_attend(cache, q)
+    with pytest.raises(ValueError, match="gradient"):
+        kv.kvcrush_cache_write(cache, k, k.detach())
+    with pytest.raises(ValueError, match="gradient"):
+        kv.make_cache(c.tensors["k"].requires_grad_(), c.tensors["v"], 20)
+    with torch.no_grad():
+        kv.kvcrush_cache_write(cache, k, k)
+        out, _ = kv.kvcrush_attend(cache, q)
+    assert torch.isfinite(out).all() and not out.requires_grad
+    with pytest.raises(ValueError, match="shape"):
+        kv.kvcrush_attend(cache, q.detach(), out=torch.empty(1, 4, 2, 64, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(ValueError, match="blocks"):
+        kv.kvcrush_attend(cache, q.detach(), blocks=torch.zeros(1, 1, 1, 4, dtype=torch.int32, device="cuda"), unit=16)
+    with pytest.raises(ValueError, match="mask"):
+        kv.kvcrush_attend(cache, q.detach(), mask=torch.zeros(1, 2, 1, dtype=torch.int64, device="cuda"))
+    with pytest.raises(kv.KVCrushError):
+        kv.kvcrush_attend(cache, q.detach().half())
+
+
+@pytest.mark.parametrize("n_new,lengths", [([3, 3], [2, 40]), ([-5, 100], [30, 3]), ([2 ** 31 - 1, -2 ** 31], [10, 10])])
+def test_counts_and_lengths_outside_their_ranges_are_pulled_into_them(n_new, lengths):
+    """n_new beyond T or the length, negative ones, lengths beyond S: as the header says, clamped."""
+    B, T, D = 2, 3, 64
+    c = ref.Case("i8", B, 2, lengths, D, capacity=64, seed=6).cuda()
+    given = torch.tensor([L if L != 40 else 10 ** 9 for L in lengths], dtype=torch.int32, device="cuda")
+    cache = kv.make_cache(c.tensors["k"], c.tensors["v"], max(lengths), c.tensors["k_param"], c.tensors["v_param"], given)
+    q = values((B, 4, T, D), "bf16", 8)
+    real = [min(max(n, 0), T, L) for n, L in zip(n_new, lengths)]
+    counts = torch.tensor(n_new, dtype=torch.int32, device="cuda")
+    check_attention(c, q, kv.kvcrush_attend(cache, q.cuda(), n_new=counts), real)
+    bnd = kv.kvcrush_block_bounds(cache, 8)
+    got = kv.kvcrush_block_select(cache, q.cuda(), *bnd, 8, 3, 1, 1, n_new=counts)
+    assert torch.equal(got.cpu(), padded(reference_lists(c, q, reference_bounds(c, 8), 8, 3, 1, 1, real), 3))
+
+
+def test_block_tables_that_name_blocks_outside_the_pool():
+    """Such entries are pulled into the pool, never followed: results are those of the pulled table."""
+    c = ref.Case("bf16", 1, 2, [60], 64, block_size=16, seed=2)
+    n = c.n_blocks
+    good = torch.tensor([[0, n - 1, 1, n - 1]], dtype=torch.int32)
+    bad = torch.tensor([[-7, n, 1, 2 ** 31 - 1]], dtype=torch.int32)
+    c.tensors = {w: None if t is None else torch.nan_to_num(t, nan=0.5) for w, t in c.tensors.items()}
+    c.cuda()
+    q = values((1, 4, 1, 64), "bf16", 3).cuda()
+    results = []
+    for table in (good, bad):
+        cache = kv.make_cache(c.tensors["k"], c.tensors["v"], 60, block_table=table.cuda())
+        results.append((*kv.kvcrush_attend(cache, q), *kv.kvcrush_cache_read(cache), *kv.kvcrush_block_bounds(cache, 8)))
+    for a, b in zip(*results):
+        assert torch.equal(bits(a), bits(b))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "i4"])
+def test_sequences_of_very_different_lengths_share_the_pieces(fmt):
+    """Lengths on the device, many sequences: pieces dealt by length, some sequences with one piece, empty ones among them."""
+    lengths = [4000, 1, 0, 700, 33, 2500, 5, 64] + [7] * 13
+    B = len(lengths)
+    c = ref.Case(fmt, B, 1, lengths, 64, seed=5).cuda()
+    q = values((B, 4, 2, 64), "bf16", 4)
+    check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [min(2, x) for x in lengths])
+
+
+def test_more_sequences_than_a_wave_has_lanes():
+    lengths = [(37 * i) % 300 for i in range(70)]
+    c = ref.Case("i8", 70, 1, lengths, 64, seed=5).cuda()
+    q = values((70, 2, 1, 64), "f16", 4)
+    check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [min(1, x) for x in lengths])
