@@ -571,3 +571,32 @@ def test_more_sequences_than_a_wave_has_lanes():
     c = ref.Case("i8", 70, 1, lengths, 64, seed=5).cuda()
     q = values((70, 2, 1, 64), "f16", 4)
     check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [min(1, x) for x in lengths])
+
+
+@pytest.mark.parametrize("fmt,rows", [("i8", 2_400_000), ("bf16", 1_200_000)])
+def test_offsets_beyond_32_bits(fmt, rows):
+    """A pool of more than 4 GiB whose last blocks are used."""
+    D, Hkv, bs = 128, 16, 4
+    n_blocks = rows // bs
+    k, v = (torch.zeros(n_blocks, bs, Hkv, D, dtype=ref.STORED[fmt], device="cuda") for _ in range(2))
+    assert k.numel() * k.element_size() > 2 ** 32
+    k_param, v_param = (torch.zeros(n_blocks, bs, Hkv, device="cuda") if fmt == "i8" else None for _ in range(2))
+    table = torch.tensor([[n_blocks - 1, 0, n_blocks - 2, n_blocks // 2 + 1]], dtype=torch.int32)
+    cache = kv.make_cache(k, v, 13, k_param, v_param, block_table=table.cuda())
+    new = {w: values((1, Hkv, 13, D), "bf16", i) for i, w in enumerate("kv")}
+    kv.kvcrush_cache_write(cache, new["k"].cuda(), new["v"].cuda())
+    c = ref.Case(fmt, 1, Hkv, [13], D)
+    for w in "kv":
+        x = new[w].float().numpy()
+        codes, par = (x, None) if fmt == "bf16" else ref.quantise(x, fmt)
+        c.rows64[w] = ref.values64(codes, par, fmt)
+    q = values((1, 32, 1, D), "bf16", 9)
+    check_attention(c, q, kv.kvcrush_attend(cache, q.cuda()), [1])
+    got = kv.kvcrush_cache_read(cache, dtype=torch.bfloat16)
+    for w, x in zip("kv", got):
+        assert (np.abs(x.cpu().double().numpy() - c.rows64[w]) <= 2.0 ** -8 * np.abs(c.rows64[w])).all()
+    tokens = lambda t: torch.stack([t[int(table[0, i // bs]), i % bs] for i in range(12)]).transpose(0, 1)  # noqa: E731
+    bnd = kv.kvcrush_block_bounds(cache, 4)
+    par = None if fmt == "bf16" else tokens(k_param).cpu().numpy()
+    want = ref.bounds(ref.values32(ref.load(tokens(k), fmt), par, fmt), 12, 4, 3)
+    assert np.array_equal(bnd[0][0, :, :3].cpu().numpy(), want[0]) and np.array_equal(bnd[1][0, :, :3].cpu().numpy(), want[1])
