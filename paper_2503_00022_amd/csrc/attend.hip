@@ -367,9 +367,10 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   // row_wave + RW, ..  in_tile: this lane's bytes of a piece, in a tile whose rows lie one behind the other.
   constexpr int kOwn = 2 * F::kLoads / RW;
   static_assert(2 * F::kLoads % RW == 0, "the waves of a group copy alike");
-  uint32_t in_tile[kOwn];
+  constexpr int kOffsets = F::kLoads / RW > 0 ? F::kLoads / RW : 1;  // (K's pieces and V's lie alike)
+  uint32_t in_tile[kOffsets];
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) {
+  for (int j = 0; j < kOffsets; ++j) {
     int row, chunk;
     F::chunk_of((j * RW + row_wave) % F::kLoads * 64 + lane, row, chunk);
     in_tile[j] = row * F::kRow + chunk * 16;
@@ -415,13 +416,14 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         const size_t from = (row_base + k0) * F::kRow;
         const char *k = kvc::tiles::wave_uniform(p.c.k + from), *v = kvc::tiles::wave_uniform(p.c.v + from);
 #pragma unroll
-        for (int j = 0; j < kOwn; ++j) copy16<ONCE>(j * RW + row_wave < F::kLoads ? k : v, in_tile[j], dst + j * RW * 1024);
+        for (int j = 0; j < kOwn; ++j) copy16<ONCE>(j * RW + row_wave < F::kLoads ? k : v, in_tile[j % kOffsets], dst + j * RW * 1024);
       } else {
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
-          const int row = in_tile[j] / F::kRow;
+          const uint32_t at = in_tile[j % kOffsets];
+          const int row = at / F::kRow;
           const int tok = lookup ? places[ahead + row] & 0x7FFFFFFF : min(k0 + row, L - 1);
-          const size_t from = (row_base + (size_t)tok * row_step) * F::kRow + in_tile[j] % F::kRow;
+          const size_t from = (row_base + (size_t)tok * row_step) * F::kRow + at % F::kRow;
           copy16<ONCE>((j * RW + row_wave < F::kLoads ? p.c.k : p.c.v) + from, dst + j * RW * 1024);
         }
       }
