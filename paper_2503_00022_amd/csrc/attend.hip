@@ -928,14 +928,14 @@ kvcrush_status make_plan(const kvcrush_cache* c, const kvcrush_attend_args* a, P
   });
   const long long most = std::max(1ll, std::min<long long>((keys + step - 1) / step, kMaxSplit));
   // Time of n pieces a sequence, in us as measured at both ends: 4 for a workgroup and 1.5 for each tile of its waves, in
-  // rounds of one workgroup to a compute unit; 3.5 to merge pieces.  (2 sequences of 160 keys in one piece, 11.4, or two,
-  // 14.2; 8 of 2048 in four, 18.6, or one, 32.)
+  // rounds of one workgroup to a compute unit; 5 to merge pieces (3.5 on the chip, and the host launches for 3.4 as well).
+  // 2 sequences of 160 keys in one piece each take 10.4, in two 14.2; 8 of 2048 in one 32, in four 18.6.
   const long long workgroups = base * c->B, steps = (keys + step - 1) / step;
   const long long n_end = std::min(most, 2 * kUnits / workgroups + 1);
   double least = 0.0;
   plan.n_split = 1;
   for (long long n = 1; n <= n_end; ++n) {
-    const double us = (double)((workgroups * n + kUnits - 1) / kUnits) * (4.0 + 1.5 * (double)((steps + n - 1) / n)) + (n > 1 ? 3.5 : 0.0);
+    const double us = (double)((workgroups * n + kUnits - 1) / kUnits) * (4.0 + 1.5 * (double)((steps + n - 1) / n)) + (n > 1 ? 5.0 : 0.0);
     if (n > 1 && us >= 0.97 * least) continue;
     least = us;
     plan.n_split = (int)n;
