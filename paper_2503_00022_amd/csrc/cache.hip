@@ -3,7 +3,10 @@
 // Both directions are bound by the bytes they move (a value of 2 or 4 bytes on one side, 1 or 1/2 on the
 // other).  Eight neighbouring values of a row belong to one lane, so that a row is D / 8 = 8 or 16 lanes
 // whose extremes are combined by DPP moves, a wave moves four or eight rows with one 16-byte load a lane,
-// and kRows of those are in flight together.
+// and kRows of those are in flight together (one where there are few rows: a single token's 128 rows take 2.9 us,
+// a launch's latency).  The side in values is used once and passes the caches by: 8 x 8192 tokens of 8 heads into a
+// paged e4m3 cache 90 -> 73 us (5.6 TB/s), four e4m3 caches of up to 7839 tokens back 40 -> 26 (6.1 TB/s, part of the codes
+// from the last-level cache).
 #include <algorithm>
 
 #include "cache.h"
