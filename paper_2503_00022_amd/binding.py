@@ -530,12 +530,15 @@ def _rows(t, name: str, index: int):
 
 def _strides(t):
     """Element strides of [B,H,T,D] (sequence, head, token), None if packed; an axis of one element has any stride, so its
-    packed one is given."""
+    packed one is given.  Three zeros are the library's sign for packed: refused."""
     if t.is_contiguous():
         return None
     B, H, T, D = t.shape
     st = t.stride()
-    return st[0] if B > 1 else H * T * D, st[1] if H > 1 else T * D, st[2] if T > 1 else D
+    st = st[0] if B > 1 else H * T * D, st[1] if H > 1 else T * D, st[2] if T > 1 else D
+    if st == (0, 0, 0):
+        raise ValueError("one row expanded to all sequences, heads and tokens: pass its contiguous() copy")
+    return st
 
 
 def _stride_array(t):
@@ -580,7 +583,7 @@ def _hand_over(stream, *made):
 
 
 def kvcrush_cache_write(cache: Cache, k_new, v_new, n_new=None, stream=None):
-    """k_new, v_new [B,Hkv,T,D] (any strides, D contiguous) become the last T tokens of their sequences: the cache's
+    """k_new, v_new [B,Hkv,T,D] (any strides but three zeros, D contiguous) become the last T tokens of their sequences: the cache's
     lengths count them already.  n_new int32 [B]: only the first n_new[b] of sequence b's are real.  Quantised caches
     take float32, bfloat16 and float16, the others their own type."""
     index, shape = cache.index, k_new.shape
@@ -647,7 +650,7 @@ def _queries(cache, q):
 
 def kvcrush_attend(cache: Cache, q, mask=None, n_new=None, blocks=None, unit=0, scale=0.0, out=None, lse=None, workspace=None,
                    stream=None):
-    """The newest T tokens, whose rows are in the cache, attend to it: q [B,Hq,T,D] (any strides, D contiguous) ->
+    """The newest T tokens, whose rows are in the cache, attend to it: q [B,Hq,T,D] (any strides but three zeros, D contiguous) ->
     (out like q, lse float32 [B,Hq,T], the rows' natural log-sum-exps).
     mask: int64 words [B,T,ceil(T/64)], or [T,ceil(T/64)] for all sequences: bit j % 64 of word j / 64 of row t lets new
     token t see new token j; without it, those up to itself.  All tokens before the new ones are seen.

@@ -2,7 +2,7 @@
 // own type or quantised, over all of it or over listed blocks.
 //
 // The queries of all heads of a KV group and of all new tokens are the rows that one key serves: R = T * G of
-// them.  A wave takes kTile keys at a time and 16 NC of those rows (NC = 1, 2, 4):
+// them.  A wave takes kTile keys at a time and 16 NC of those rows (NC = 1 or 2; RW waves share the tiles):
 //   S^T = K Q^T      keys x rows, 16x16 matrix instructions: a lane holds one row's logits, of every fourth group of
 //                    four keys
 //   softmax          one reference exponent and one sum per row in registers

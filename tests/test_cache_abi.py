@@ -158,6 +158,16 @@ def test_block_refusals(lib):
     assert select(unit=1, ws=None) == WORKSPACE and select(unit=1, ws_bytes=need - 1) == WORKSPACE and select(unit=1, ws=ODD) == WORKSPACE
 
 
+def test_one_row_for_all_is_not_taken_for_a_packed_tensor():
+    """Three zero strides mean packed to the library, which would read far behind the row."""
+    row = torch.zeros(1, 1, 1, 64)
+    with pytest.raises(ValueError, match="contiguous"):
+        kv._strides(row.expand(2, 3, 4, 64))
+    assert kv._strides(row.expand(2, 3, 1, 64)) == (0, 0, 64)       # an axis of one element has its packed stride
+    assert kv._strides(row.expand(1, 3, 4, 64)) == (3 * 4 * 64, 0, 0)
+    assert kv._strides(row) is None
+
+
 def test_binding_refuses_host_memory_and_wrong_shapes():
     k = torch.zeros(2, 2, 32, 64, dtype=torch.int8)
     with pytest.raises(ValueError, match="GPU memory"):
