@@ -472,7 +472,7 @@ kvcrush_status kvcrush_attend(const kvcrush_cache* cache, const kvcrush_attend_a
  * Nb = ceil(capacity / unit).  Only the blocks that hold one of the last T tokens (of the n real ones, with
  * n_new) are computed, the others stay as they are; T = 0: every block of the sequence.  Keys are assumed
  * finite.
- * Size limits: unit <= 1024, B * Hkv <= 65535. */
+ * Size limits: unit <= 1024, Nb <= 2^25, B * Hkv <= 65535. */
 kvcrush_status kvcrush_block_bounds(const kvcrush_cache* cache, int32_t unit, int32_t T, const int32_t* n_new,
                                     int8_t* bounds, float* scales, void* hip_stream);
 
@@ -485,7 +485,7 @@ kvcrush_status kvcrush_block_bounds(const kvcrush_cache* cache, int32_t unit, in
  *   bounds, scales  as kvcrush_block_bounds leaves them
  *   blocks  [B, Hkv, T, n_select] int32: ascending; -1 where the sequence has no more blocks, and for padding
  * Of args only Hq, T, dtype, q_stride and n_new are read (dtype may be any of q's types on any cache).
- * Size limits: ceil(S / unit) <= 32768, Hq / Hkv <= 1024, B * Hkv <= 65535, B * Hkv * T <= 2^21;
+ * Size limits: ceil(S / unit) and n_select <= 32768, Hq / Hkv <= 1024, B * Hkv <= 65535, B * Hkv * T <= 2^21;
  * 0 <= n_sink + n_recent <= n_select. */
 size_t kvcrush_block_select_workspace(const kvcrush_cache* cache, const kvcrush_attend_args* args, int32_t unit,
                                       int32_t n_select);

@@ -26,6 +26,7 @@ struct BoundsParams {
 };
 
 constexpr int kBoundWaves = 4;
+constexpr int kMostBounds = 1 << 25;  // blocks of a sequence: a grid's axis stays below 2^32 threads
 
 // A wave takes one block: D / 8 lanes a row, 64 / (D / 8) rows at a time.
 template <int FORMAT, int D>
@@ -313,7 +314,7 @@ kvcrush_status select_ok(const kvcrush_cache* c, const kvcrush_attend_args* a, i
     return KVCRUSH_ERR_INVALID_ARG;
   if (a->T > 1024 || a->Hq / c->Hkv > 1024 || (long long)c->B * c->Hkv > 65535 || (long long)c->B * c->Hkv * a->T > (1 << 21))
     return KVCRUSH_ERR_UNSUPPORTED;
-  if (((long long)c->S + unit - 1) / unit > kMaxBlocks) return KVCRUSH_ERR_UNSUPPORTED;
+  if (((long long)c->S + unit - 1) / unit > kMaxBlocks || n_select > kMaxBlocks) return KVCRUSH_ERR_UNSUPPORTED;
   return KVCRUSH_OK;
 }
 
@@ -330,7 +331,8 @@ extern "C" kvcrush_status kvcrush_block_bounds(const kvcrush_cache* cache, int32
   kvcrush_status st = check(cache);
   if (st != KVCRUSH_OK) return st;
   if (unit < 1 || T < 0) return KVCRUSH_ERR_INVALID_ARG;
-  if (unit > 1024 || (long long)cache->B * cache->Hkv > 65535) return KVCRUSH_ERR_UNSUPPORTED;
+  if (unit > 1024 || (long long)cache->B * cache->Hkv > 65535 || blocks_of(cache->capacity, unit) > kMostBounds)
+    return KVCRUSH_ERR_UNSUPPORTED;
   if (!bounds || !scales || !kvc::aligned16(bounds) || !kvc::aligned16(scales)) return KVCRUSH_ERR_INVALID_ARG;
   if (cache->S == 0) return KVCRUSH_OK;
   BoundsParams p;

@@ -146,6 +146,9 @@ def test_block_refusals(lib):
 
     assert bounds(unit=0) == INVALID and bounds(T=-1) == INVALID and bounds(b=None) == INVALID and bounds(s=ODD) == INVALID
     assert bounds(unit=1025) == UNSUPPORTED and bounds(cache(B=70000)) == UNSUPPORTED
+    big = dict(base=dict(GOOD, B=1, Hkv=1, S=0, capacity=1 << 29))                  # 2^26 and 2^25 blocks
+    assert bounds(cache(**big), unit=8) == UNSUPPORTED and bounds(cache(**big), unit=16) == OK
+    assert select(n=32769) == UNSUPPORTED and select(n=2 ** 31 - 1) == UNSUPPORTED
     assert bounds(cache(S=0)) == OK                                               # an empty cache has no blocks
     assert select(unit=0) == INVALID and select(n=0) == INVALID and select(sink=-1) == INVALID and select(sink=3, recent=2) == INVALID
     assert select(sink=2 ** 31 - 1, recent=2 ** 31 - 1) == INVALID
