@@ -221,7 +221,7 @@ class KVCache:
         if format is not None:
             self.k_param, self.v_param = (new(*rows, *((2,) if format == "i4" else ()), dtype=torch.float32) for _ in range(2))
         self.lengths, self.block_table = new(B, dtype=torch.int32), block_table
-        self.capacity, self.dtype, self.unit, self.scale, self.bound = capacity, dtype, unit, scale, 0
+        self.capacity, self.dtype, self.unit, self.scale = capacity, dtype, unit, scale
         self.cache = kv.make_cache(self.k, self.v, 0, self.k_param, self.v_param, self.lengths, block_table)
         self.bounds = self.bound_scales = None
         if unit:
@@ -229,29 +229,36 @@ class KVCache:
             self.bounds, self.bound_scales = new(B, Hkv, nb, 2, D, dtype=torch.int8), new(B, Hkv, nb, dtype=torch.float32)
         self._ws = {}
 
+    bound = property(lambda self: self.cache.S, lambda self, n: setattr(self.cache, "S", n),
+                     doc="No sequence is longer than this: the calls read up to it, whatever `lengths` says.")
+
     def append(self, k_new, v_new, n_new=None):
-        """k_new, v_new [B,Hkv,T,D]: T tokens more for every sequence, or the first n_new[b] (int32 [B] on the GPU) of them.
-        A sequence must not outgrow the capacity (the caller's to see to where n_new decides)."""
+        """k_new, v_new [B,Hkv,T,D]: T tokens more for every sequence, or the first n_new[b] (int32 [B] on the GPU, 0 to T)
+        of them.  A sequence must not outgrow the capacity (the caller's to see to where n_new decides)."""
         T = k_new.shape[2]
         if n_new is None and self.bound + T > self.capacity:
             raise ValueError(f"{T} tokens more may pass the capacity of {self.capacity}: set `bound` to the longest length")
-        before = self.bound, self.cache.S
-        self.bound = self.cache.S = min(self.bound + T, self.capacity)
         self.lengths.add_(T if n_new is None else n_new)
+        before, self.bound = self.bound, min(self.bound + T, self.capacity)
         try:
             kv.kvcrush_cache_write(self.cache, k_new, v_new, n_new=n_new)
+            if not self.k.is_inference():
+                increment_version((self.k, self.v))  # (a backward pass that saved the cache is to notice)
             if self.unit:
                 kv.kvcrush_block_bounds(self.cache, self.unit, self.bounds, self.bound_scales, T=T, n_new=n_new)
         except Exception:   # (a refused call leaves the cache as long as it was)
             self.lengths.sub_(T if n_new is None else n_new)
-            self.bound, self.cache.S = before
+            self.bound = before
             raise
 
     def drop(self, n):
-        """The last n tokens (a number, or int32 [B] on the GPU) of every sequence are taken back, as rejected drafts are."""
-        self.lengths.sub_(n)
+        """The last n tokens (a number, or int32 [B] on the GPU, not negative) of every sequence are taken back, as rejected
+        drafts are; a sequence that has fewer is empty then."""
+        if isinstance(n, int) and n < 0:
+            raise ValueError("n must not be negative")
+        self.lengths.sub_(n).clamp_(min=0)
         if isinstance(n, int):
-            self.bound = self.cache.S = max(self.bound - n, 0)
+            self.bound = max(self.bound - n, 0)
 
     def attend(self, q, mask=None, n_new=None, n_select=0, n_sink=1, n_recent=1):
         """The last T tokens attend to the cache: q [B,Hq,T,D], mask and n_new as kvcrush_attend takes them -> (out, lse).

@@ -168,6 +168,45 @@ def test_a_refused_append_leaves_the_cache():
         c.attend(values((1, 2, 1, 64), 1).cuda(), n_select=2)
 
 
+@pytest.mark.gpu
+def test_lengths_and_their_bound():
+    """A bound that is set counts for every call; a drop of more than there is empties; a refused count changes nothing."""
+    c = KVCache(2, 2, 64, 64)
+    x = values((2, 2, 20, 64), 1).cuda()
+    c.append(x, x)
+    c.bound = 8
+    assert c.read()[0].shape[2] == 8 and torch.equal(c.read()[0], x[:, :, :8])
+    c.bound = 20
+    with pytest.raises(RuntimeError):
+        c.append(x, x, n_new=torch.ones(3, dtype=torch.int32, device="cuda"))
+    assert c.bound == 20 and c.lengths.tolist() == [20, 20]
+    with pytest.raises(ValueError, match="negative"):
+        c.drop(-1)
+    c.drop(torch.tensor([30, 4], dtype=torch.int32, device="cuda"))
+    assert c.lengths.tolist() == [0, 16] and c.bound == 20
+    c.append(x[:, :, :3], x[:, :, :3])
+    assert c.lengths.tolist() == [3, 19] and c.bound == 23
+    k = c.read()[0]
+    assert torch.equal(k[0, :, :3], x[0, :, :3]) and torch.equal(k[1, :, :19], torch.cat([x[1, :, :16], x[1, :, :3]], 1))
+    assert not k[0, :, 3:].any() and not k[1, :, 19:].any()
+    c.drop(40)
+    assert c.lengths.tolist() == [0, 0] and c.bound == 0
+    out, lse = c.attend(values((2, 4, 1, 64), 2).cuda())
+    assert not out.any() and (lse == -float("inf")).all()
+
+
+@pytest.mark.gpu
+def test_a_backward_pass_notices_an_append():
+    c = KVCache(1, 2, 16, 64)
+    x = values((1, 2, 3, 64), 1).cuda()
+    c.append(x, x)
+    w = torch.ones_like(c.k, requires_grad=True)
+    y = (w * c.k).sum()
+    c.append(x, x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
 def test_arguments_that_do_not_fit():
     with pytest.raises(ValueError, match="format"):
         KVCache(1, 1, 32, 64, format="fp4", device="cpu")
