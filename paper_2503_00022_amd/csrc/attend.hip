@@ -16,9 +16,10 @@
 // Measured: 8 sequences of 2048 bf16 keys, 67 MB, 17 us (4.0 TB/s; 22 where they come from memory and not from the
 // last-level cache) and 4 to merge; 4 paged e4m3 caches of up to 32768 keys, 225 MB, 55 to 58 us (4.1 TB/s; 3 to 8 of them
 // until the first tiles are there); 64 rows over 16384 bf16 keys 25 us, of which a tile of 32 keys takes 2.5 on eight waves
-// and the first one, with the code still to be fetched, 5; 256 rows over 2 x 7839 8-bit keys 45 us, 510 vector instructions
-// (24 us of issue) and 48 matrix instructions (9 us) a wave and tile of 32 rows: bound by the former, of which a third
-// makes halves of codes.
+// and the first one, with the code still to be fetched, 5; 256 rows over 2 x 7839 8-bit keys 41 us, a wave and
+// tile of 32 rows being 510 vector instructions and 48 matrix instructions: those issue in 60 % of the time, these take 20,
+// and the rest is the way through the LDS and the barriers.  (Halves of the codes made once for the four waves that share a
+// tile: a fifth fewer vector instructions, one more way through the LDS, no faster.)
 #include <algorithm>
 #include <cmath>
 
@@ -76,8 +77,9 @@ struct Fmt {
   // Eight waves where LDS and registers have room for them: two to a SIMD, so that one's matrix instructions run beside
   // the other's arithmetic.  RW of them share a tile.
   static constexpr int lds(int waves, int RW) { return waves / RW * stages(RW) * kStage + waves * kAhead * 4; }
-  // Groups of waves that meet at a barrier look two tiles ahead where there is room.
-  static constexpr int stages(int RW) { return RW > 1 && 8 / RW * 3 * kStage + 8 * kAhead * 4 <= kvc::kLdsPerWorkgroup ? 3 : 2; }
+  // Groups of waves that share tiles meet at a barrier for every second one where there is room for two pairs (256 rows over
+  // 2 x 7839 8-bit keys: a barrier a tile 53.5 us, every second 48.5, every fourth 48.9).
+  static constexpr int stages(int RW) { return RW > 1 && 8 / RW * 4 * kStage + 8 * kAhead * 4 <= kvc::kLdsPerWorkgroup ? 4 : 2; }
   static constexpr int waves(int NC, int RW) {
     return (NC == 2 && kBits == 4) || lds(8, RW) > kvc::kLdsPerWorkgroup ? 4 : 8;
   }
@@ -311,8 +313,8 @@ __device__ __forceinline__ Deal deal(const AttendParams& p, int step) {
 }
 
 // RW: waves that share a tile, each with 16 NC rows of its own.  One: the waves are on their own, and nobody waits for
-// another's copies.  More: they copy a share each and meet at a barrier per tile, so that many rows cost one reading of
-// the keys.
+// another's copies.  More: they copy a share each and meet at a barrier every kMeet tiles, so that many rows cost one
+// reading of the keys.
 template <class F, int NC, int RW>
 __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(AttendParams p) {
   constexpr int kWaves = F::waves(NC, RW), kGroups = kWaves / RW, kStages = F::stages(RW);
@@ -383,6 +385,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     in_tile[j] = row * F::kRow + chunk * 16;
   }
   constexpr int kCopies = kOwn + F::kParamLoads;
+  constexpr int kMeet = kStages / 2;  // tiles from one barrier to the next (RW > 1)
   auto issue = [&](int tile) {
     const int k0 = tile * kTile, i = tile - tile0, ahead = (i * kTile) & (kAhead - 1);
     const uint32_t stage = own_at + (i % kStages) * F::kStage, dst = stage + row_wave * 1024;
@@ -456,7 +459,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     }
   };
 #pragma unroll
-  for (int i = 0; i < (RW > 1 ? kStages - 1 : kStages); ++i)
+  for (int i = 0; i < (RW > 1 ? kMeet : kStages); ++i)
     if (tile0 + i < tile1) issue(tile0 + i);
 
   // ---- this lane's rows, and the queries as the first product's other operand
@@ -527,14 +530,14 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   for (int turn = 0; turn < (RW > 1 ? per_group : tile1 - tile0); ++turn) {
     const int tile = tile0 + turn, k0 = tile * kTile;
     if constexpr (RW > 1) {
-      // behind the barrier the group's copies of this tile are all done, and so are its reads of the one before
-      if (kStages == 3 && tile + 1 < tile1)
-        wait_copies<kCopies>();
-      else
+      // behind the barrier the group's copies of the next kMeet tiles are all done, and so are its reads of those before
+      if (turn % kMeet == 0) {
         wait_copies<0>();
-      wait_reads();
-      __syncthreads();
-      if (tile + kStages - 1 < tile1) issue(tile + kStages - 1);
+        wait_reads();
+        __syncthreads();
+        for (int i = kMeet; i < kStages; ++i)
+          if (tile + i < tile1) issue(tile + i);
+      }
       if (tile >= tile1) continue;  // (the last group may have a tile less)
     } else {
       if (turn > 0) {
