@@ -16,7 +16,7 @@
 // Measured: 8 sequences of 2048 bf16 keys, 67 MB, 17 us (4.0 TB/s; 22 where they come from memory and not from the
 // last-level cache) and 4 to merge; 4 paged e4m3 caches of up to 32768 keys, 225 MB, 55 to 58 us (4.1 TB/s; 3 to 8 of them
 // until the first tiles are there); 64 rows over 16384 bf16 keys 25 us, of which a tile of 32 keys takes 2.5 on eight waves
-// and the first one, with the code still to be fetched, 5; 256 rows over 2 x 7839 8-bit keys 41 us, a wave and
+// and the first one, with the code still to be fetched, 5; 256 rows over 2 x 7839 8-bit keys 43 us, a wave and
 // tile of 32 rows being 510 vector instructions and 48 matrix instructions: those issue in 60 % of the time, these take 20,
 // and the rest is the way through the LDS and the barriers.  (Halves of the codes made once for the four waves that share a
 // tile: a fifth fewer vector instructions, one more way through the LDS, no faster.)
@@ -527,6 +527,9 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     for (int d = 0; d < F::kDTiles; ++d) o[c][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
+  // The two waves of a SIMD (wave, wave + 4) leave a barrier together: one goes ahead, so that its matrix instructions run
+  // beside the other's arithmetic (256 rows of 8-bit keys 48.9 -> 48.2 us, 64 of bfloat16 27.4 -> 27.2).
+  if (RW > 1 && wave >= 4) __builtin_amdgcn_s_setprio(2);
   for (int turn = 0; turn < (RW > 1 ? per_group : tile1 - tile0); ++turn) {
     const int tile = tile0 + turn, k0 = tile * kTile;
     if constexpr (RW > 1) {
