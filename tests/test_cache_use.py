@@ -276,6 +276,19 @@ def test_long_caches_in_pieces(fmt, B, Hq, Hkv, lengths, T, D, block_size):
     assert torch.equal(bits(got[0]), bits(again[0])) and torch.equal(got[1], again[1])
 
 
+@pytest.mark.parametrize("fmt,B,Hq,Hkv,lengths,T,D", [
+    ("i8", 1, 21, 3, [1500], 101, 64), ("bf16", 3, 14, 2, [900, 40, 700], 51, 128), ("f32", 1, 27, 3, [600], 77, 128),
+    ("i4", 2, 30, 2, [0, 1400], 71, 64)])
+def test_pieces_of_many_rows(fmt, B, Hq, Hkv, lengths, T, D):
+    """More than 2048 rows, no multiple of a workgroup's, whose pieces each group of lanes merges by itself: equal cuts of one
+    sequence, cuts by length of several, sequences that have no piece to merge."""
+    assert B * Hq * T > 2048 and B * Hq * T % 8
+    c = ref.Case(fmt, B, Hkv, lengths, D, seed=T, room=70).cuda()
+    q, cache = values((B, Hq, T, D), q_type(fmt), 5).cuda(), c.make(kv)
+    assert kv.kvcrush_attend_workspace(cache, Hq, T, q.dtype) > 0
+    check_attention(c, q, kv.kvcrush_attend(cache, q), [min(T, n) for n in lengths])
+
+
 # ---------------------------------------------------------------------------------------------- blocks
 def reference_bounds(c, unit):
     nb = -(-c.capacity // unit)
