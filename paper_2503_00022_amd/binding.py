@@ -519,6 +519,12 @@ def _packed(t, name: str, index: int, dtype, shape):
     return t.data_ptr()
 
 
+def _scratch(t, index: int):
+    _here(t, "workspace", index)
+    if not t.is_contiguous():   # (its nbytes are what the library may write from its first one on)
+        raise ValueError("workspace must be contiguous")
+
+
 def _rows(t, name: str, index: int):
     """[B,H,T,D] on the cache's device with the D values contiguous (any other strides)."""
     _here(t, name, index)
@@ -686,7 +692,7 @@ def kvcrush_attend(cache: Cache, q, mask=None, n_new=None, blocks=None, unit=0, 
     if workspace is None:
         workspace = made_ws = torch.empty(max(L.kvcrush_attend_workspace(cache, args), 16), dtype=torch.uint8, device=cache.device)
     else:
-        _here(workspace, "workspace", index)
+        _scratch(workspace, index)
     with _Device(index):
         st = L.kvcrush_attend(cache, args, q.data_ptr(), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                               _stream_of(cache, stream))
@@ -750,7 +756,7 @@ def kvcrush_block_select(cache: Cache, q, bounds, scales, unit: int, n_select: i
         need = L.kvcrush_block_select_workspace(cache, args, unit, n_select)
         workspace = made_ws = torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
     else:
-        _here(workspace, "workspace", index)
+        _scratch(workspace, index)
     with _Device(index):
         st = L.kvcrush_block_select(cache, args, unit, n_select, n_sink, n_recent, q.data_ptr(), bounds_at, scales_at,
                                     blocks.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(cache, stream))

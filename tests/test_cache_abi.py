@@ -171,6 +171,15 @@ def test_one_row_for_all_is_not_taken_for_a_packed_tensor():
     assert kv._strides(row) is None
 
 
+def test_scratch_memory_is_as_large_as_it_says():
+    one = torch.zeros(1, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="contiguous"):
+        kv._scratch(one.expand(1 << 20), one.get_device())
+    with pytest.raises(ValueError, match="GPU memory"):
+        kv._scratch(one, 0)
+    kv._scratch(one, one.get_device())
+
+
 def test_binding_refuses_host_memory_and_wrong_shapes():
     k = torch.zeros(2, 2, 32, 64, dtype=torch.int8)
     with pytest.raises(ValueError, match="GPU memory"):
