@@ -85,6 +85,7 @@ struct Fmt {
   }
   static constexpr int kSteps = D / 32;            // matrix steps of 32 values along D (16-bit operands)
   static constexpr int kDTiles = D / 16;
+  static constexpr int kVTerms = FORMAT == KVCRUSH_F16 ? 2 : 1;  // bfloat16 values that one of V is the sum of
   static_assert(kTileBytes % 1024 == 0, "whole wave instructions");
 
   // XOR on a 16-byte chunk's place in its 256-byte line of the tile's image, by the line's number.  Two reads must find
@@ -109,7 +110,7 @@ struct Fmt {
   }
 };
 
-// C += A B^T for one step of 32 values along the inner axis; operands are halves unless the cache is bfloat16.
+// C += A B^T for one step of 32 values along the inner axis; operands are bfloat16 or halves.
 template <int FORMAT>
 __device__ __forceinline__ void mma(f32x4& c, const u32x4& a, const u32x4& b) {
   if constexpr (FORMAT == KVCRUSH_BF16)
@@ -137,6 +138,9 @@ __device__ __forceinline__ float row_sum(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
+
+// A float without what lies below its eighth bit.
+__device__ __forceinline__ float first8(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 
 // Keys: register r of group u of lane group g = lane / 16 holds key 16 u + 4 g + r; element e of a step of 32 keys is
 // register e % 4 of group e / 4.
@@ -179,27 +183,37 @@ __device__ __forceinline__ int step_value(int g, int t) {
   return F::kChunks == 4 ? g * 32 + t * 8 : g * 16 + t * 8;
 }
 
-// V^T's operand of 16 values (tile dt) x 32 keys (step ks): lane = value, its eight keys step_key(g, e).
+// V^T's operand of 16 values (tile dt) x 32 keys (step ks) as bfloat16: lane = value, its eight keys step_key(g, e).
+// A half is the sum of two, exactly: its first eight bits and the three that are left.
 template <class F>
-__device__ __forceinline__ u32x4 v_frag(const char* tile, int lane, int dt, int ks) {
+__device__ __forceinline__ void v_frag(const char* tile, int lane, int dt, int ks, u32x4 (&f)[F::kVTerms]) {
   const int g = lane >> 4, i = lane & 15;
   if constexpr (F::kBits == 16) {
     const int row = 32 * ks + 4 * g + (i >> 2), chunk = dt * 2 + ((i & 3) >> 1), off = (i & 1) * 8;
     const u32x2 a = read_tr16(tile + F::chunk_at(row, chunk) + off), b = read_tr16(tile + F::chunk_at(row + 16, chunk) + off);
-    return u32x4{a[0], a[1], b[0], b[1]};
+    f[0] = u32x4{a[0], a[1], b[0], b[1]};
+    if constexpr (F::FORMAT == KVCRUSH_F16) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f16x2 h = as_f16x2(f[0][j]);
+        const float x = (float)h[0], y = (float)h[1];
+        f[0][j] = upper2(x, y);
+        f[1][j] = upper2(x - first8(x), y - first8(y));
+      }
+    }
   } else {
     static_assert(F::kBits == 8, "");
     const int row = 32 * ks + step_key(g, i >> 1);
     const u32x2 w = read_tr8(tile + F::chunk_at(row, dt) + (i & 1) * 8);
-    const u32x2 a = codes4_to_f16<F::FORMAT>(w[0]), b = codes4_to_f16<F::FORMAT>(w[1]);
-    return u32x4{a[0], a[1], b[0], b[1]};
+    const u32x2 a = codes4_to_bf16<F::FORMAT>(w[0]), b = codes4_to_bf16<F::FORMAT>(w[1]);
+    f[0] = u32x4{a[0], a[1], b[0], b[1]};
   }
 }
-// 4-bit codes of 64 keys: one word a step.  codes8_to_f16's order is undone by the order of the rows.
+// 4-bit codes of 64 keys: one word a step.  codes8_to_bf16's order is undone by the order of the rows.
 template <class F>
 __device__ __forceinline__ u32x2 v_codes4(const char* tile, int lane, int dt) {
   const int g = lane >> 4, i = lane & 15, j = i & 7;
-  const int row = 32 * (i >> 3) + step_key(g, j < 4 ? 2 * j : 2 * j - 7);
+  const int row = 32 * (i >> 3) + step_key(g, (j >> 1) + 4 * (j & 1));
   return read_tr4(tile + F::chunk_at(row, dt >> 1) + (dt & 1) * 8);
 }
 
@@ -515,9 +529,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
 
   f32x4 o[NC][F::kDTiles];
   // Reference exponent m (base 2) of a row: o, l and z are sums of 2^(logit - m).  It need not be the largest logit: it is
-  // raised, and the sums brought to it, only where a product of probability and V's scale could pass 2^8 (scales below
-  // 2^-88 counting as that, so that no probability passes 2^96): what is rounded to 16 bits lies in their range, and few
-  // tiles pay for it.
+  // raised, and the sums brought to it, only where a probability would pass 2^8, so that few tiles pay for it.
   float m[NC], l[NC], z[NC];  // l: sum of this lane's keys; z: sum of probability x lowest value
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
@@ -594,19 +606,12 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
       }
     }
     f32x4 v_scale[U], v_low[U];
-    float above[NC];  // log2 of the largest scale of V that this lane's keys have, -88 at least
     if constexpr (F::kQuant) {
-      float top = 0.0f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         v_scale[u] = *(const f32x4*)(vp + 16 * u + 4 * g);
         if constexpr (FORMAT == KVCRUSH_I4) v_low[u] = *(const f32x4*)(vp + 2 * kTile + 16 * u + 4 * g);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, v_scale[u][r]);
       }
-      top = fmaxf(__builtin_amdgcn_logf(top), -88.0f);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) above[c] = top;
     }
     uint32_t seen[NC] = {};  // bit 4 u + r: this row sees the key (where it is looked at)
     if (look) {
@@ -637,15 +642,9 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         see = t_of[c] < n ? (see | old) & there : 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) seen[c] |= (uint32_t)(see >> (16 * u + 4 * g) & 15) << (4 * u);
-        // (a logit or a scale that the row does not see may be anything)
-        float top = 0.0f;
+        // (a logit that the row does not see may be anything)
 #pragma unroll
-        for (int i = 0; i < 4 * U; ++i) {
-          const bool it = (seen[c] >> i) & 1;
-          s[c][i / 4][i % 4] = it ? s[c][i / 4][i % 4] : -__builtin_inff();
-          if constexpr (F::kQuant) top = fmaxf(top, it ? v_scale[i / 4][i % 4] : 0.0f);
-        }
-        if constexpr (F::kQuant) above[c] = fmaxf(__builtin_amdgcn_logf(top), -88.0f);
+        for (int i = 0; i < 4 * U; ++i) s[c][i / 4][i % 4] = (seen[c] >> i) & 1 ? s[c][i / 4][i % 4] : -__builtin_inff();
       }
     }
 
@@ -656,7 +655,6 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
 #pragma unroll
       for (int i = 1; i < 4 * U; ++i) most = fmaxf(most, s[c][i / 4][i % 4]);
       most *= col_scale[c];
-      if constexpr (F::kQuant) most += above[c];
       if (__ballot(most - m[c] > 8.0f) != 0) {
         const float mn = fmaxf(m[c], row_max(most)), a = __builtin_amdgcn_exp2f(m[c] - mn);
         m[c] = mn;
@@ -741,30 +739,21 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         }
       }
     } else {
-      // A weight is the sum of two 16-bit values, its rounding and what that left: rounded once, it would cost the result
-      // about as much again as its own rounding (measured: 1.4 times the error).
-      constexpr int P = FORMAT == KVCRUSH_BF16 ? KVCRUSH_BF16 : KVCRUSH_F16;
-      u32x4 hi[NC][U / 2], lo[NC][U / 2];
+      // A weight is the sum of three bfloat16, exactly and whatever its size: its first eight bits, the next and the last.
+      // (Halves, of which two would do near the largest weight, end at 2^-24.)
+      constexpr int kTerms = 3;
+      u32x4 w[NC][U / 2][kTerms];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 2 * U; ++i) {
           float x = s[c][i / 2][2 * (i % 2)], y = s[c][i / 2][2 * (i % 2) + 1];
-          // (values from here on: otherwise the compiler may round the product behind x to 16 bits in one step for
-          // `hi` and in two for what `hi` left)
-          asm("" : "+v"(x), "+v"(y));
-          const uint32_t both = pack2<P>(x, y);
-          float xh, yh;
-          if constexpr (P == KVCRUSH_BF16) {
-            xh = __uint_as_float(both << 16);
-            yh = __uint_as_float(both & 0xFFFF0000u);
-          } else {
-            const f16x2 f = as_f16x2(both);
-            xh = (float)f[0];
-            yh = (float)f[1];
+#pragma unroll
+          for (int j = 0; j < kTerms; ++j) {
+            w[c][i / 4][j][i % 4] = upper2(x, y);
+            x -= first8(x);
+            y -= first8(y);
           }
-          hi[c][i / 4][i % 4] = both;
-          lo[c][i / 4][i % 4] = pack2<P>(__builtin_fmaf(xh, -1.0f, x), __builtin_fmaf(yh, -1.0f, y));
         }
 #pragma unroll
       for (int d = 0; d < F::kDTiles; ++d) {
@@ -772,16 +761,18 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         if constexpr (F::kBits == 4) codes = v_codes4<F>(vt, lane, d);
 #pragma unroll
         for (int ks = 0; ks < U / 2; ++ks) {
-          u32x4 vf;
+          u32x4 vf[F::kVTerms];
           if constexpr (F::kBits == 4)
-            vf = codes8_to_f16(codes[ks]);
+            vf[0] = codes8_to_bf16(codes[ks]);
           else
-            vf = v_frag<F>(vt, lane, d, ks);
+            v_frag<F>(vt, lane, d, ks, vf);
+          // (the last bits of both together are below 2^-24 of the product)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            mma<FORMAT>(o[c][d], vf, hi[c][ks]);
-            mma<FORMAT>(o[c][d], vf, lo[c][ks]);
-          }
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < F::kVTerms; ++i)
+#pragma unroll
+              for (int j = 0; i + j < kTerms; ++j) mma<KVCRUSH_BF16>(o[c][d], vf[i], w[c][ks][j]);
         }
       }
     }

@@ -174,6 +174,30 @@ __device__ __forceinline__ u32x2 codes4_to_f16(uint32_t w) {
     return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
   }
 }
+// Two floats' upper halves: as bfloat16, cut off below their eighth bit (exact where there is nothing below).
+__device__ __forceinline__ uint32_t upper2(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// Four 8-bit codes as bfloat16, exactly.
+template <int FORMAT>
+__device__ __forceinline__ u32x2 codes4_to_bf16(uint32_t w) {
+  if constexpr (FORMAT == KVCRUSH_E4M3) {
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))};
+  } else {
+    auto code = [&](int i) { return (float)(int)(int8_t)(w >> (8 * i)); };
+    return u32x2{upper2(code(0), code(1)), upper2(code(2), code(3))};
+  }
+}
+// Eight 4-bit codes as bfloat16, exactly, in the order 0 2 4 6 1 3 5 7.  (As an 8-bit float of 3 mantissa bits, a byte
+// below 16 stands for itself times 2^-9.)
+__device__ __forceinline__ u32x4 codes8_to_bf16(uint32_t w) {
+  const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.0f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, 512.0f, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, true))};
+}
 // Eight 4-bit codes as halves, exactly, in the order 0 4 1 5 2 6 3 7.
 __device__ __forceinline__ u32x4 codes8_to_f16(uint32_t w) {
   const f16x2 off = {(_Float16)-1024.0f, (_Float16)-1024.0f};
