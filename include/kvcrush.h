@@ -439,7 +439,8 @@ kvcrush_status kvcrush_cache_read(const kvcrush_cache* cache, int32_t n, const i
  * Accuracy: products of the cache's values as they stand (a quantised row's parameters are applied in
  * fp32), fp32 sums.  Queries on a quantised cache enter as halves scaled by their row's largest value (a value
  * below 2^-29 of it loses bits); a probability, times V's scale, enters the second product with all 24 bits of
- * its fp32 value, however small it is beside the others (above 2^-102; below, its last bits may be lost).
+ * its fp32 value (8-bit formats: to 2^-18 of it), however small it is beside the others (above 2^-102; below, its
+ * last bits may be lost).
  */
 typedef struct {
   int32_t Hq;            /* query heads, a multiple of Hkv; head h reads KV head h / (Hq / Hkv)     */

@@ -739,20 +739,25 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         }
       }
     } else {
-      // A weight is the sum of three bfloat16, exactly and whatever its size: its first eight bits, the next and the last.
-      // (Halves, of which two would do near the largest weight, end at 2^-24.)
-      constexpr int kTerms = 3;
+      // A weight is the sum of bfloat16 values, whatever its size: its rounding, that of what is left, and what is left then.
+      // (Halves end at 2^-24.)  Three are the weight, exactly; with two, off by 2^-18 of it, 8-bit values make do (256 rows
+      // over 2 x 7839 keys 49 us, with three 55).  4-bit ones do not: the codes' sum and the lowest values' cancel.
+      constexpr int kTerms = F::kBits == 8 ? 2 : 3;
       u32x4 w[NC][U / 2][kTerms];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 2 * U; ++i) {
           float x = s[c][i / 2][2 * (i % 2)], y = s[c][i / 2][2 * (i % 2) + 1];
+          // (values from here on: otherwise the compiler may round the product behind x in one step for a term and in two
+          // for what it left)
+          asm("" : "+v"(x), "+v"(y));
 #pragma unroll
           for (int j = 0; j < kTerms; ++j) {
-            w[c][i / 4][j][i % 4] = upper2(x, y);
-            x -= first8(x);
-            y -= first8(y);
+            const uint32_t both = pack2<KVCRUSH_BF16>(x, y);
+            w[c][i / 4][j][i % 4] = both;
+            x -= __uint_as_float(both << 16);
+            y -= __uint_as_float(both & 0xFFFF0000u);
           }
         }
 #pragma unroll
@@ -766,7 +771,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
             vf[0] = codes8_to_bf16(codes[ks]);
           else
             v_frag<F>(vt, lane, d, ks, vf);
-          // (the last bits of both together are below 2^-24 of the product)
+          // (what is left of both is below 2^-25 of the product)
 #pragma unroll
           for (int c = 0; c < NC; ++c)
 #pragma unroll
