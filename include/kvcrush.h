@@ -434,8 +434,9 @@ kvcrush_status kvcrush_cache_read(const kvcrush_cache* cache, int32_t n, const i
  *   mask, those up to itself.
  *   out[b, h, t] = sum_j softmax_j(scale q . K[j]) V[j]     lse[b, h, t] = ln sum_j exp(scale q . K[j])
  * over what it sees.  A query that sees nothing and one that is padding get out = 0, lse = -infinity.
- * What a query does not see has no influence on its result, whatever it holds; rows at and beyond a
- * sequence's length are not read at all.
+ * What a query does not see has no influence on its result, whatever it holds; what it sees counts as it is,
+ * infinities, NaN and values near fp32's largest included (such calls take many times as long).  Rows at and beyond
+ * a sequence's length are not read at all.
  * Accuracy: products of the cache's values as they stand (a quantised row's parameters are applied in
  * fp32), fp32 sums.  Queries on a quantised cache enter as halves scaled by their row's largest value (a value
  * below 2^-29 of it loses bits); a probability, times V's scale, enters the second product with all 24 bits of

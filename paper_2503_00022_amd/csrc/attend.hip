@@ -217,26 +217,6 @@ __device__ __forceinline__ u32x2 v_codes4(const char* tile, int lane, int dt) {
   return read_tr4(tile + F::chunk_at(row, dt >> 1) + (dt & 1) * 8);
 }
 
-template <int FORMAT>
-__device__ __forceinline__ bool all_finite(uint32_t w) {  // the values in one word
-  if constexpr (FORMAT == KVCRUSH_F32) return (w & 0x7F800000u) != 0x7F800000u;
-  if constexpr (FORMAT == KVCRUSH_BF16) return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
-  if constexpr (FORMAT == KVCRUSH_F16) return (w & 0x7C00u) != 0x7C00u && (w & 0x7C000000u) != 0x7C000000u;
-  w &= 0x7F7F7F7Fu;  // e4m3: 0x7F is NaN
-  return (w & 255u) != 127u && ((w >> 8) & 255u) != 127u && ((w >> 16) & 255u) != 127u && (w >> 24) != 127u;
-}
-// Value d of row `key` of V's tile, as it enters the second product.
-template <class F>
-__device__ __forceinline__ float tile_value(const char* tile, int key, int d) {
-  const int at = d * F::kBits / 8;
-  const char* p = tile + F::chunk_at(key, at >> 4) + (at & 15);
-  if constexpr (F::FORMAT == KVCRUSH_F32) return *(const float*)p;
-  if constexpr (F::FORMAT == KVCRUSH_BF16) return __uint_as_float((uint32_t) * (const uint16_t*)p << 16);
-  if constexpr (F::FORMAT == KVCRUSH_F16) return (float)*(const _Float16*)p;
-  const u32x2 h = codes4_to_f16<F::FORMAT>(*(const uint8_t*)p);
-  return (float)as_f16x2(h[0])[0];
-}
-
 // Position of a key slot, and whether there is a token (without branches, so that many are looked up at a time).
 struct Slots {
   const int32_t* list;  // this query's blocks, or null
@@ -250,6 +230,16 @@ struct Slots {
     return there & (pos < L);
   }
 };
+
+// The slots of query t (without lists: of every query), n of whose sequence's T new tokens are real.
+__device__ __forceinline__ Slots key_slots(const AttendParams& p, int b, int h, int t, int n) {
+  Slots s;
+  s.L = p.c.length(b);
+  s.list = p.blocks ? p.blocks + ((size_t)(b * p.c.Hkv + h) * p.T + t) * p.n_list : nullptr;
+  s.unit = p.unit;
+  s.n = p.blocks ? (t < n ? p.n_list * p.unit : 0) : n > 0 ? s.L : 0;
+  return s;
+}
 
 // Asynchronous copies into LDS, 16 or 4 bytes a lane to `dst` + 16 or 4 x lane (dst uniform).  Written out, so that the
 // compiler does not wait for all of them before each LDS read that follows; whoever reads waits with wait_copies and
@@ -281,11 +271,18 @@ __device__ __forceinline__ void wait_copies() {  // until at most LEFT of this w
 }
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// Four values of a row, from its sums: out = sum / total, lse = m + log2 total.
-__device__ __forceinline__ void store_result(const AttendParams& p, int b, int head, int t, int e, float m, float total, f32x4 sum) {
+// Sums of several waves, then of several pieces are added up as these fractions of themselves: eight, and kMaxSplit, of the
+// largest numbers that fp32 has stay below it.
+constexpr int kMaxSplit = 256;
+constexpr float kWaveRoom = 0x1p-4f, kPieceRoom = 0x1p-9f;
+// 2^x for x <= 0, the factor of what a row has seen; never 0, so that an infinity stays one.
+__device__ __forceinline__ float factor(float x) { return fmaxf(__builtin_amdgcn_exp2f(x), 0x1p-149f); }
+
+// Four values of a row, from its sums: out = sum / room / total, lse = m + log2 total.
+__device__ __forceinline__ void store_result(const AttendParams& p, int b, int head, int t, int e, float m, float total, f32x4 sum, float room) {
   if (p.lse && e == 0)
     p.lse[((size_t)b * p.Hq + head) * p.T + t] = total == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(total)) * kLn2;
-  const float inv = 1.0f / total;
+  const float inv = 1.0f / room / total;
   float x[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = total == 0.0f ? 0.0f : sum[i] * inv;
@@ -296,6 +293,107 @@ __device__ __forceinline__ void store_result(const AttendParams& p, int b, int h
     *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_BF16>(x[0], x[1]), pack2<KVCRUSH_BF16>(x[2], x[3])};
   else
     *(u32x2*)(p.out + at * 2) = u32x2{pack2<KVCRUSH_F16>(x[0], x[1]), pack2<KVCRUSH_F16>(x[2], x[3])};
+}
+
+// Some rows over the key slots from `first` to `last`, key by key and without the matrix cores: for what they get wrong.  A
+// value that is not finite must reach the rows that see its key, as it is, and no others (0 x NaN; an infinity times the
+// terms of a weight, some of them 0, is NaN), and the product of a very large one with a weight above 1 is not finite.  Here
+// a row's weights add up to less than 1.  Rare, so written to be short: with an infinity among the keys, 8 sequences of 2048
+// bf16 keys take 40 us, 64 rows over 16384 keys 340, 256 rows over 2 x 7839 1.5 ms.
+constexpr int kTogether = 4;
+template <int D>
+struct Sums {
+  float m[kTogether], l[kTogether], sum[kTogether][8];  // sum: values 8 (lane % (D / 8)) .. + 7
+};
+template <int FORMAT, int D>
+__device__ __forceinline__ Sums<D> key_by_key(int b, int h, int t_list, int n, const int (&rows)[kTogether], int first, int last) {
+  // (the kernel's arguments once more from where they were: kept in registers for this, they cost every call)
+  auto at = (const __attribute__((address_space(4))) AttendParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  const AttendParams p = *(const AttendParams*)at;
+  constexpr int kLanes = D / 8, kKeys = KVC_WAVE / kLanes;  // lanes of a key, keys of a load
+  const int lane = kvc::lane_id(), chunk = lane % kLanes, first_new = p.c.length(b) - n;
+  const Slots slots = key_slots(p, b, h, t_list, n);
+  last = min(last, slots.n);
+  const size_t base = p.c.base(b, h), step = p.c.step();
+  const float scale = fmaxf(p.scale_log2, 0x1p-100f), room = (float)(33 - __builtin_clz(max(last - first, 1)));
+  Sums<D> y;
+  float q[kTogether][8];
+  int t_of[kTogether];
+#pragma unroll
+  for (int r = 0; r < kTogether; ++r) {
+    const int t = p.blocks ? t_list : rows[r] / p.G, head = h * p.G + (p.blocks ? rows[r] : rows[r] - t * p.G);
+    const char* from = p.q + ((size_t)b * p.q_stride[0] + (size_t)head * p.q_stride[1] + (size_t)t * p.q_stride[2] + chunk * 8) * (format_bits(p.q_dtype) / 8);
+    if (p.q_dtype == KVCRUSH_F32)
+      load8<KVCRUSH_F32>(from, q[r]);
+    else if (p.q_dtype == KVCRUSH_BF16)
+      load8<KVCRUSH_BF16>(from, q[r]);
+    else
+      load8<KVCRUSH_F16>(from, q[r]);
+    t_of[r] = t;
+    y.m[r] = kNegBig;
+    y.l[r] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y.sum[r][j] = 0.0f;
+  }
+#pragma unroll 1
+  for (int k0 = first; k0 < last; k0 += KVC_WAVE) {
+    int pos;
+    const bool there = slots.position(k0 + lane, pos) & (k0 + lane < last);
+    const int draft = pos - first_new, token = p.c.token(b, there ? pos : 0);
+    float x[kTogether] = {};
+#pragma unroll 4
+    for (int i = 0; i < kLanes; ++i) {
+      float k[8];
+      row_values<FORMAT>(p.c.k, p.c.k_param, base + (size_t)__shfl(token, i * kKeys + lane / kLanes) * step, D, chunk * 8, k);
+#pragma unroll
+      for (int r = 0; r < kTogether; ++r) {
+        float part = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part = __builtin_fmaf(q[r][j], k[j], part);
+#pragma unroll
+        for (int off = 1; off < kLanes; off *= 2) part += __shfl_xor(part, off);
+        part = __shfl(part, lane % kKeys * kLanes);
+        x[r] = i == lane / kKeys ? part : x[r];
+      }
+    }
+    float weight[kTogether];
+    uint64_t seen[kTogether];
+#pragma unroll
+    for (int r = 0; r < kTogether; ++r) {
+      const uint64_t* words = p.mask ? p.mask + (size_t)b * p.mask_stride + (size_t)t_of[r] * p.mask_words : nullptr;
+      const bool see = there & (draft < 0 || (words ? (words[min(max(draft >> 6, 0), p.mask_words - 1)] >> (draft & 63)) & 1 : draft <= t_of[r]));
+      const float v = see ? x[r] * scale : -__builtin_inff(), mn = fmaxf(y.m[r], kvc::wave_max(v) + room), a = factor(y.m[r] - mn);
+      y.m[r] = mn;
+      weight[r] = v - mn > -__builtin_inff() ? factor(v - mn) : __builtin_amdgcn_exp2f(v - mn);  // (0, NaN as they are)
+      y.l[r] = y.l[r] * a + weight[r];
+      seen[r] = __ballot(see);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y.sum[r][j] *= a;
+    }
+#pragma unroll 4
+    for (int i = 0; i < kLanes; ++i) {
+      const int key = i * kKeys + lane / kLanes;
+      float v[8];
+      row_values<FORMAT>(p.c.v, p.c.v_param, base + (size_t)__shfl(token, key) * step, D, chunk * 8, v);
+#pragma unroll
+      for (int r = 0; r < kTogether; ++r) {
+        const float w = __shfl(weight[r], key);
+        const bool it = (seen[r] >> key) & 1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y.sum[r][j] = it ? __builtin_fmaf(w, v[j], y.sum[r][j]) : y.sum[r][j];
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kTogether; ++r) {
+    y.l[r] = kvc::wave_sum(y.l[r]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int off = kLanes; off < KVC_WAVE; off *= 2) y.sum[r][j] += __shfl_xor(y.sum[r][j], off);
+  }
+  return y;
 }
 
 // The cut of the sequences' keys into p.pieces pieces of `size` steps of `step` keys, in order of the sequences, each with
@@ -355,7 +453,6 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     piece_tiles = d.size * kGroups;
     if (blockIdx.x == 0 && tid < p.c.B) p.cuts[tid] = make_int2(d.first, d.n);
   }
-  const int bh = b * p.c.Hkv + h;
   const int L = p.c.length(b), n = new_tokens(p.n_new, b, p.T, L);
   // with lists, a query's G heads are the rows
   constexpr int kRows = 16 * NC * RW;
@@ -364,11 +461,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   const int row0 = (p.blocks ? row_tile % tiles_of_query : row_tile) * kRows;
   const int rows = p.blocks ? p.G : p.G * p.T;
 
-  Slots slots;
-  slots.list = p.blocks ? p.blocks + ((size_t)bh * p.T + t_list) * p.n_list : nullptr;
-  slots.unit = p.unit;
-  slots.n = p.blocks ? (t_list < n ? p.n_list * p.unit : 0) : n > 0 ? L : 0;
-  slots.L = L;
+  const Slots slots = key_slots(p, b, h, t_list, n);
 
   // this wave's (or its group's) tiles: a contiguous piece of the workgroup's
   const int tiles = (slots.n + kTile - 1) / kTile, per_wg = piece_tiles > 0 ? piece_tiles : (tiles + n_split - 1) / n_split;
@@ -690,42 +783,6 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         }
       }
     }
-    if constexpr (FORMAT != KVCRUSH_I8 && FORMAT != KVCRUSH_I4) {
-      if (look) {
-        // A value that is not finite must not reach the rows that do not see its key (0 x NaN): the keys of a tile
-        // with one are added one by one, each to the rows that see it.
-        bool odd = false;
-#pragma unroll
-        for (int j = 0; j < F::kLoads; ++j) {
-          const u32x4 x = *(const u32x4*)(vt + j * 1024 + lane * 16);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) odd = odd || !all_finite<FORMAT>(x[i]);
-        }
-        if (__ballot(odd) != 0) {
-#pragma unroll 1
-          for (int key = 0; key < kTile; ++key) {
-            const int reg = 4 * (key >> 4) + (key & 3), from = col + 16 * ((key >> 2) & 3);
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              float x = 0.0f;
-#pragma unroll
-              for (int i = 0; i < 4 * U; ++i) x = i == reg ? s[c][i / 4][i % 4] : x;
-              x = __shfl(x, from);
-              if (__shfl((int)((seen[c] >> reg) & 1), from)) {
-#pragma unroll
-                for (int d = 0; d < F::kDTiles; ++d) {
-#pragma unroll
-                  for (int r = 0; r < 4; ++r) o[c][d][r] += x * tile_value<F>(vt, key, d * 16 + 4 * g + r);
-                  asm volatile("" : : : "memory");  // (few values at a time: no registers for what is rare)
-                }
-              }
-            }
-          }
-          continue;
-        }
-      }
-    }
-
     // ---- values
     if constexpr (F::kBits == 32) {
 #pragma unroll
@@ -787,19 +844,54 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
   constexpr int kPitch = D + 4;
   float2* ml = (float2*)lds_all;                                    // [waves][NC][16]
   float* sums = (float*)(lds_all + kWaves * NC * 128);              // [waves][16][kPitch]
+  uint64_t bad = 0;  // bit 16 c + col: a row of this wave whose sums are not finite
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     l[c] = row_sum(l[c]);
-    if constexpr (FORMAT == KVCRUSH_I4) {
-      z[c] = row_sum(z[c]);
+    if constexpr (FORMAT == KVCRUSH_I4) z[c] = row_sum(z[c]);
+    float check = 0.0f;  // NaN as soon as one value is not finite
 #pragma unroll
-      for (int d = 0; d < F::kDTiles; ++d)
+    for (int d = 0; d < F::kDTiles; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[c][d][r] += z[c];
-    }
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (FORMAT == KVCRUSH_I4) o[c][d][r] += z[c];
+        check = __builtin_fmaf(o[c][d][r], 0.0f, check);
+      }
     if (t_of[c] >= n) {  // padding: it sees nothing
       l[c] = 0.0f;
       m[c] = kNegBig;
+    }
+    const bool stored = row0 + (row_wave * NC + c) * 16 + col < rows && t_of[c] < n;
+    const uint64_t rows_of = __ballot(check != 0.0f && stored);
+    bad |= ((rows_of | rows_of >> 16 | rows_of >> 32 | rows_of >> 48) & 0xFFFF) << (16 * c);
+  }
+  // The rows whose sums are not finite are done again.  (Nothing is asked of the values in the loop above: a test of each
+  // tile would cost every call.)
+#pragma unroll 1
+  while (bad != 0) {
+    int at[kTogether], of[kTogether];  // which of the wave's rows, and of all
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+      at[i] = bad != 0 ? __builtin_ctzll(bad) : at[0];
+      of[i] = row0 + row_wave * NC * 16 + at[i];
+      bad &= bad - 1;
+    }
+    const Sums<D> y = key_by_key<FORMAT, D>(b, h, t_list, n, of, tile0 * kTile, tile1 * kTile);
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+#pragma unroll
+      for (int d = 0; d < F::kDTiles; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float even = __shfl(y.sum[i][r], 2 * d + (g >> 1)), odd = __shfl(y.sum[i][4 + r], 2 * d + (g >> 1));
+#pragma unroll
+          for (int c = 0; c < NC; ++c) o[c][d][r] = 16 * c + col == at[i] ? (g & 1 ? odd : even) : o[c][d][r];
+        }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        l[c] = 16 * c + col == at[i] ? y.l[i] : l[c];
+        m[c] = 16 * c + col == at[i] ? y.m[i] : m[c];
+      }
     }
   }
   __syncthreads();
@@ -812,11 +904,11 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     float top = kNegBig;
 #pragma unroll
     for (int x = 0; x < kGroups; ++x) top = fmaxf(top, ml[((x * RW + row_wave) * NC + c) * 16 + col].x);
-    const float a = __builtin_amdgcn_exp2f(m[c] - top);
+    const float a = factor(m[c] - top);
     if (c > 0) __syncthreads();
 #pragma unroll
     for (int d = 0; d < F::kDTiles; ++d)
-      *(f32x4*)(sums + (wave * 16 + col) * kPitch + d * 16 + 4 * g) = f32x4{o[c][d][0] * a, o[c][d][1] * a, o[c][d][2] * a, o[c][d][3] * a};
+      *(f32x4*)(sums + (wave * 16 + col) * kPitch + d * 16 + 4 * g) = o[c][d] * kWaveRoom * a;
     __syncthreads();
     // four values a thread
     for (int i = tid; i < RW * 16 * (D / 4); i += kWaves * KVC_WAVE) {
@@ -839,7 +931,7 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
         if (e == 0) p.part_ml[at] = make_float2(most, total);
         *(f32x4*)(p.part_o + at * D + e) = sum;
       } else {
-        store_result(p, b, head, t, e, most, total, sum);
+        store_result(p, b, head, t, e, most, total, sum, kWaveRoom);
       }
     }
   }
@@ -871,10 +963,10 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
   for (int i = part; i < n; i += ALONE ? 1 : kGroups) {
     const float2 x = p.part_ml[at + i * pitch];
     const f32x4 y = *(const f32x4*)(p.part_o + (at + i * pitch) * D + e);
-    const float mn = fmaxf(m, x.x), a = __builtin_amdgcn_exp2f(m - mn), c = __builtin_amdgcn_exp2f(x.x - mn);
+    const float mn = fmaxf(m, x.x), a = factor(m - mn), c = factor(x.x - mn);
     m = mn;
     total = total * a + x.y * c;
-    sum = sum * a + y * c;
+    sum = sum * a + y * kPieceRoom * c;
   }
   if constexpr (!ALONE) {
     sums[part][e / 4] = sum;
@@ -885,13 +977,13 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(AttendParams p) {
     for (int i = 1; i < kGroups; ++i) {
       const float2 x = mls[i];
       const f32x4 y = sums[i][e / 4];
-      const float mn = fmaxf(m, x.x), a = __builtin_amdgcn_exp2f(m - mn), c = __builtin_amdgcn_exp2f(x.x - mn);
+      const float mn = fmaxf(m, x.x), a = factor(m - mn), c = factor(x.x - mn);
       m = mn;
       total = total * a + x.y * c;
       sum = sum * a + y * c;
     }
   }
-  store_result(p, b, head, t, e, m, total, sum);
+  store_result(p, b, head, t, e, m, total, sum, kWaveRoom * kPieceRoom);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -901,7 +993,6 @@ struct Plan {
   long long rows;  // B * Hq * T
 };
 
-constexpr int kMaxSplit = 256;
 // Keys that one workgroup reads each, and that are more than half of the last-level cache's 256 MB holds, pass the caches
 // by: nothing of them is left there for the next step.  (225 MB: 61 -> 57 us; 67 MB, which do stay: 18.6 -> 20.0.  Where
 // row tiles or queries share keys, 6 % slower.)

@@ -73,3 +73,101 @@ def test_one_large_row_that_hardly_counts(fmt, orders, rows):
     c = made(fmt, k, v)
     q = torch.ones(1, Hq, T, D).to(ref.DTYPES[q_type(fmt, "f16")])
     check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [T])
+
+
+def near_or_alike(c, q, got, n_new, seen=None):
+    """check_attention where the formula's results are finite, and its infinities and NaN elsewhere."""
+    out = got[0].cpu().double().numpy()
+    with np.errstate(invalid="ignore"):
+        want = ref.attend(q.double().numpy(), c.rows64["k"], c.rows64["v"], c.lengths, n_new, seen)[0]
+    odd = ~np.isfinite(want)
+    assert odd.any() and np.array_equal(out[odd], want[odd], equal_nan=True)
+    rows = {w: c.rows64[w].copy() for w in "kv"}
+    plain = np.isfinite(c.rows64["v"])
+    c.rows64["v"] = np.where(plain, c.rows64["v"], 0.0)          # (values of other columns than those that are compared)
+    out[odd] = ref.attend(q.double().numpy(), c.rows64["k"], c.rows64["v"], c.lengths, n_new, seen)[0][odd]
+    check_attention(c, q, (torch.from_numpy(out), got[1]), n_new, seen)
+    c.rows64 = rows
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("block_size", [0, 16])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("L,D,orders", [(150, 128, 0), (150, 64, 5), (2500, 128, 130)])
+def test_infinities_and_nan_reach_the_rows_that_see_them(fmt, block_size, rows, L, D, orders):
+    """In old keys (all rows see them) and in drafts (some do): infinities of both signs, NaN, at keys of ordinary weight
+    (orders = 0) and far below the largest."""
+    Hq, Hkv, T = rows
+    rng = np.random.RandomState(L + T)
+    k, v = (rng.randn(1, Hkv, L, D).astype(np.float32) for _ in range(2))
+    bad = [3, L // 2, L - 1] + ([L - T + 1] if T > 2 else [])
+    k[:, :, bad[:2]] = -orders * math.log(2) / math.sqrt(D)
+    v[:, :, bad[0], 3], v[:, :, bad[0], 7], v[:, :, bad[1], 7] = math.inf, -math.inf, -math.inf
+    v[:, :, bad[1], 9], v[:, :, bad[0], 11], v[:, :, bad[1], 11] = math.nan, math.inf, -math.inf
+    v[:, :, bad[2], 13] = math.inf
+    if T > 2:
+        v[:, :, bad[3], 15], v[:, 0, bad[3], 17] = -math.inf, math.nan
+    seen = ref.tree(T, rng, roots=0.5)[None]
+    c = made(fmt, k, v, block_size)
+    q = torch.ones(1, Hq, T, D).to(ref.DTYPES[fmt])
+    got = kv.kvcrush_attend(c.make(kv), q.cuda(), mask=ref.mask_words(seen).cuda())
+    near_or_alike(c, q, got, [T], seen)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "i8", "i4"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("which", ["k", "v", "old"])
+def test_rows_of_nan_reach_the_rows_that_see_them(fmt, rows, which):
+    """A quantised row with a value that was not finite is NaN throughout, and so is what sees it, whole."""
+    Hq, Hkv, T = rows
+    L, D, rng = 200, 128, np.random.RandomState(T)
+    k, v = (rng.randn(1, Hkv, L, D).astype(np.float32) for _ in range(2))
+    at = 40 if which == "old" else L - T // 2 - 1
+    (k if which == "k" else v)[:, -1, at, 5] = math.inf
+    c = made(fmt, k, v)
+    seen = ref.tree(T, rng, roots=0.5)[None]
+    q = values((1, Hq, T, D), "bf16", 3)
+    out, lse = kv.kvcrush_attend(c.make(kv), q.cuda(), mask=ref.mask_words(seen).cuda())
+    sees = np.ones(T, dtype=bool) if which == "old" else seen[0, :, at - (L - T)]
+    hit = np.zeros((Hq, T), dtype=bool)
+    hit[Hq - Hq // Hkv:] = sees
+    assert np.array_equal(torch.isnan(out[0]).cpu().numpy(), np.broadcast_to(hit[..., None], (Hq, T, D)))
+    assert np.array_equal(torch.isnan(lse[0]).cpu().numpy(), hit if which == "k" else np.zeros_like(hit))
+    hurt = c.rows64["v"][:, -1, at].copy(), c.rows64["k"][:, -1, at].copy()
+    c.rows64["v"][:, -1, at] = c.rows64["k"][:, -1, at] = 0
+    want = ref.attend(q.double().numpy(), c.rows64["k"], c.rows64["v"], [L], [T], seen)
+    c.rows64["v"][:, -1, at], c.rows64["k"][:, -1, at] = hurt
+    # (the rows that do not see it: one rounding, probabilities and logits as in check_attention, some tens of them)
+    far = np.abs(out[0].cpu().double().numpy() - want[0][0])[~hit]
+    assert (far <= 2.0 ** -8 * np.abs(want[0][0][~hit]) + 2.0 ** -14 * want[2][0][~hit]).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "f32", "e4m3", "i8"])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("L,lengths", [(90, False), (2500, False), (2500, True)])
+def test_values_near_the_largest(fmt, rows, L, lengths):
+    """Columns of one large value, of its negative and of both in turn, beside small ones."""
+    Hq, Hkv, T = rows
+    D, rng = 64, np.random.RandomState(L)
+    top = 0.99 * torch.finfo(ref.DTYPES[fmt]).max if fmt in ref.DTYPES else 2.0 ** 127
+    k = (0.1 * rng.randn(2, Hkv, L, D)).astype(np.float32)
+    v = rng.randn(2, Hkv, L, D).astype(np.float32)
+    v[..., 0], v[..., 1] = top, -top
+    v[..., ::2, 2], v[..., 1::2, 2] = top, -top
+    v[:, :, 5, 3] = top
+    c = made(fmt, k, v)
+    q = torch.ones(2, Hq, T, D).to(ref.DTYPES[q_type(fmt)])
+    check_attention(c, q, kv.kvcrush_attend(c.make(kv, use_lengths=lengths), q.cuda()), [T, T])
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("level", [2.0 ** 40, -1e30, 2.0 ** 127])
+def test_rows_without_a_range(rows, level):
+    """4-bit rows of one value each: no scale, all of it in the lowest value."""
+    Hq, Hkv, T = rows
+    D, L, rng = 128, 300, np.random.RandomState(3)
+    k = (0.1 * rng.randn(1, Hkv, L, D)).astype(np.float32)
+    v = np.broadcast_to(np.float32(level) * rng.uniform(0.5, 1, (1, Hkv, L, 1)).astype(np.float32), k.shape).copy()
+    c = made("i4", k, v)
+    q = torch.ones(1, Hq, T, D).bfloat16()
+    check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [T])

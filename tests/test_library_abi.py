@@ -169,6 +169,16 @@ def test_short_prompt_and_decoding_kernels_keep_their_registers():
         assert "mfma" not in name or (r["Occupancy"] >= 4 and r["LDS Size"] <= 80 * 1024), (name, r)
 
 
+def test_attention_kernels_keep_their_vector_registers():
+    """Each wave's sums, weights and queries stay in registers, but for a few of single precision with 64 shared rows."""
+    from paper_2503_00022_amd import build
+    attend = {n: r for n, r in build.resource_usage("attend.hip").items() if "attend_kernel" in n}
+    assert len(attend) == 48, sorted(attend)       # 6 formats x {D = 64, 128} x {16, 32, 64 shared, 128 shared} rows
+    for name, r in attend.items():
+        most = 16 if "FmtILi0ELi128E" in name and "Li2ELi2E" in name else 0
+        assert r["VGPRs Spill"] <= most, (name, r)
+
+
 def test_struct_layouts_match_the_header(tmp_path):
     """The ctypes mirrors of the header's structs have the C compiler's sizes and
     field offsets (a C program that includes the header prints them)."""
