@@ -110,7 +110,7 @@ class DecodeCache:
             B, Hs, capacity, budget, n_important, bit_topk, anchor, anchor_seed, None, n_sink, n_recent, capacity)), 16),
             dtype=torch.uint8, device=dev)
         self._idx = torch.empty(B, budget, dtype=torch.int32, device=dev)
-        self._views, self._attend_ws = [None, None], None    # made by the first attend
+        self._views = [None, None]                   # made by the first attend
         self.evictions = 0
 
     k = property(lambda self: self._sets[self._cur][0])
@@ -175,13 +175,9 @@ class DecodeCache:
         view = self._views[self._cur]
         if view is None:
             view = self._views[self._cur] = kv.make_cache(self.k, self.v, self.n)
-        q = q_new.unsqueeze(2)
-        if self._attend_ws is None or self._attend_ws[0] != q_new.shape[1]:
-            view.S = self.capacity
-            need = kv.kvcrush_attend_workspace(view, q_new.shape[1], 1, q_new.dtype)
-            self._attend_ws = q_new.shape[1], torch.empty(max(need, 16), dtype=torch.uint8, device=self.k.device)
         view.S = self.n
-        out, lse = kv.kvcrush_attend(view, q, scale=self.scale, workspace=self._attend_ws[1])
+        # (scratch memory is the call's own: kept here, it would be shared by streams that attend at the same time)
+        out, lse = kv.kvcrush_attend(view, q_new.unsqueeze(2), scale=self.scale)
         return out.squeeze(2), lse.squeeze(2)
 
 
