@@ -190,8 +190,9 @@ class KVCache:
     `n_blocks` (without one, sequence b owns blocks b * capacity / block_size and following).  `unit` > 0 keeps bounds of
     blocks of that many tokens, which attend(n_select=..) chooses by.
     lengths (int32 [B] on the GPU) counts each sequence's tokens; nothing here synchronises.  The calls capture into a HIP
-    graph once each has run outside one (workspaces are made then); a graph keeps the bound on the lengths of its capture,
-    so capture with `bound` set to what the replays will need."""
+    graph once each has run outside one; a graph keeps the bound on the lengths of its capture, so capture with `bound` set
+    to what the replays will need.  attend() and read() only read: calls on several streams, or a replayed graph beside
+    them, need no order among each other (each has scratch memory of its own), only behind the append and drop before."""
 
     def __init__(self, B, Hkv, capacity, D, dtype=torch.bfloat16, *, format=None, block_size=0, block_table=None, n_blocks=0,
                  unit=0, scale=0.0, device="cuda"):
@@ -223,7 +224,6 @@ class KVCache:
         if unit:
             nb = (capacity + unit - 1) // unit
             self.bounds, self.bound_scales = new(B, Hkv, nb, 2, D, dtype=torch.int8), new(B, Hkv, nb, dtype=torch.float32)
-        self._ws = {}
 
     bound = property(lambda self: self.cache.S, lambda self, n: setattr(self.cache, "S", n),
                      doc="No sequence is longer than this: the calls read up to it, whatever `lengths` says.")
@@ -262,26 +262,11 @@ class KVCache:
         its sequence among them."""
         if n_select and not self.unit:
             raise ValueError("n_select needs a cache with a unit")
-        B, Hq, T, D = q.shape
         blocks, cache = None, self.cache
         if n_select:
-            key = "select", Hq, T, q.dtype, n_select
-            ws = self._workspace(key, lambda: kv.kvcrush_block_select_workspace(cache, Hq, T, q.dtype, self.unit, n_select))
             blocks = kv.kvcrush_block_select(cache, q, self.bounds, self.bound_scales, self.unit, n_select, n_sink, n_recent,
-                                             n_new=n_new, workspace=ws)
-        ws = self._workspace(("attend", Hq, T, q.dtype, n_select),
-                             lambda: kv.kvcrush_attend_workspace(cache, Hq, T, q.dtype, n_list=n_select, unit=self.unit))
-        return kv.kvcrush_attend(cache, q, mask=mask, n_new=n_new, blocks=blocks, unit=self.unit, scale=self.scale, workspace=ws)
-
-    def _workspace(self, key, size):
-        ws = self._ws.get(key)
-        if ws is None:   # (large enough for any length: of the sizes for all lengths, that of the capacity is the largest)
-            now, self.cache.S = self.cache.S, self.capacity
-            try:
-                ws = self._ws[key] = torch.empty(max(size(), 16), dtype=torch.uint8, device=self.lengths.device)
-            finally:
-                self.cache.S = now
-        return ws
+                                             n_new=n_new)
+        return kv.kvcrush_attend(cache, q, mask=mask, n_new=n_new, blocks=blocks, unit=self.unit, scale=self.scale)
 
     def read(self, idx=None, n=None, dtype=None):
         """Rows as values: of positions idx int32 [B,n], or the first n (default: the bound on the lengths) -> (k, v)."""
