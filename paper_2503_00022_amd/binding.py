@@ -6,6 +6,7 @@ exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -169,6 +170,23 @@ def _stream(stream=None):
     return ctypes.c_void_p(_current_raw_stream(torch.cuda.current_device()) if stream is None else stream.cuda_stream)
 
 
+_no_context = contextlib.nullcontext()
+
+
+def _memory_of(stream):
+    """In this context a call with stream= allocates what it makes: in that stream's memory.  Of the current stream's, a block
+    may come back that work still pending there reads or writes."""
+    return _no_context if stream is None else torch.cuda.stream(stream)
+
+
+def _hand_over(stream, *results):
+    """Results made in `stream`'s memory go to the caller, who uses them under the current stream."""
+    if stream is not None:
+        for t in results:
+            if t is not None:
+                t.record_stream(torch.cuda.current_stream(t.device))
+
+
 def _check(status: int, what: str):
     if status != OK:
         raise KVCrushError(status, what)
@@ -201,17 +219,20 @@ def kvcrush_scores(q, k, reduce_groups: bool, lse=None, scores=None, workspace=N
         raise ValueError("q and k must be [B,H,S,D] tensors of one dtype with matching B, S, D")
     shape = make_shape(q, k, reduce_groups, window, scale)
     Hs = shape.Hkv if reduce_groups else shape.Hq
-    if scores is None:
-        scores = torch.empty(shape.B, Hs, shape.S, dtype=torch.float32, device=q.device)
     need = kvcrush_scores_workspace(shape)
-    if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    made_scores = made_ws = None
+    with _memory_of(stream):
+        if scores is None:
+            scores = made_scores = torch.empty(shape.B, Hs, shape.S, dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = made_ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
     if lse is not None:
         lse = _dev(lse, "lse")
         if lse.dtype != torch.float32 or tuple(lse.shape) != (shape.B, shape.Hq, shape.S):
             raise ValueError("lse must be fp32 [B,Hq,S]")
     st = load().kvcrush_scores(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(lse), _ptr(_dev(scores, "scores")),
                                _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream))
+    _hand_over(stream, made_scores, made_ws)
     _check(st, "kvcrush_scores")
     return scores, workspace
 
@@ -227,13 +248,16 @@ def kvcrush_row_lse(q, k, lse_out=None, stream=None, window=0, workspace="auto",
     kvcrush_row_lse_workspace asks for)."""
     q, k = _dev_rows(q, "q"), _dev_rows(k, "k")
     shape = make_shape(q, k, False, window, scale)
-    if lse_out is None:
-        lse_out = torch.empty(shape.B, shape.Hq, shape.S, dtype=torch.float32, device=q.device)
-    if isinstance(workspace, str):
-        workspace = torch.empty(max(kvcrush_row_lse_workspace(shape), 16), dtype=torch.uint8, device=q.device)
+    made = None
+    with _memory_of(stream):
+        if lse_out is None:
+            lse_out = made = torch.empty(shape.B, shape.Hq, shape.S, dtype=torch.float32, device=q.device)
+        if isinstance(workspace, str):
+            workspace = torch.empty(max(kvcrush_row_lse_workspace(shape), 16), dtype=torch.uint8, device=q.device)
     st = load().kvcrush_row_lse(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(_dev(lse_out, "lse_out")),
                                 _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                 _stream(stream))
+    _hand_over(stream, made)
     _check(st, "kvcrush_row_lse")
     return lse_out
 
@@ -243,11 +267,14 @@ def kvcrush_pool_scores(scores, kernel: int, out=None, stream=None):
     scores = _dev(scores, "scores")
     if scores.dtype != torch.float32:
         raise ValueError("scores must be fp32")
+    made = None
     if out is None:
-        out = torch.empty_like(scores)
+        with _memory_of(stream):
+            out = made = torch.empty_like(scores)
     S = scores.shape[-1]
     st = load().kvcrush_pool_scores(scores.numel() // S, S, kernel, _ptr(scores), _ptr(_dev(out, "out")),
                                     _stream(stream))
+    _hand_over(stream, made)
     _check(st, "kvcrush_pool_scores")
     return out
 
@@ -285,18 +312,21 @@ def kvcrush_select(scores, budget, n_important, bit_topk=0, anchor="alternating"
     args = make_select_args(B, Hs, S, budget, n_important, bit_topk, anchor, anchor_seed, anchor_bits,
                             n_sink, n_recent, stride, unit)
     dev = scores.device
-    if idx is None:
-        idx = torch.empty(B, budget, dtype=torch.int32, device=dev)
-    kind = torch.empty(B, budget, dtype=torch.uint8, device=dev) if want_kind else None
+    made = None
     if unit > 1:   # one vector of Hs * unit bits per unit of the middle
         bits_shape = (B, max(S - n_sink - n_recent, 0) // unit, (Hs * unit + 63) // 64)
     else:
         bits_shape = (B, S, (Hs + 63) // 64)
-    bits = torch.empty(bits_shape, dtype=torch.int64, device=dev) if want_bits else None
-    if workspace is None:
-        workspace = torch.empty(max(kvcrush_select_workspace(args), 16), dtype=torch.uint8, device=dev)
+    with _memory_of(stream):
+        if idx is None:
+            idx = made = torch.empty(B, budget, dtype=torch.int32, device=dev)
+        kind = torch.empty(B, budget, dtype=torch.uint8, device=dev) if want_kind else None
+        bits = torch.empty(bits_shape, dtype=torch.int64, device=dev) if want_bits else None
+        if workspace is None:
+            workspace = torch.empty(max(kvcrush_select_workspace(args), 16), dtype=torch.uint8, device=dev)
     st = load().kvcrush_select(ctypes.byref(args), _ptr(scores), _ptr(idx), _ptr(kind), _ptr(bits),
                                _ptr(workspace), workspace.numel(), _stream(stream))
+    _hand_over(stream, made, kind, bits)
     _check(st, "kvcrush_select")
     return idx, kind, bits
 
@@ -338,13 +368,16 @@ def kvcrush_compact(k, v, idx, block_table=None, block_size=16, dense_shape=None
             raise ValueError("idx out of range")
         if block_table is not None and (int(block_table.min()) < 0 or int(block_table.max()) >= k.shape[0]):
             raise ValueError("block_table names a block outside the pool")
-    if k_out is None:
-        k_out = torch.empty(B, Hkv, budget, D, dtype=k.dtype, device=k.device)
-    if v_out is None:
-        v_out = torch.empty(B, Hkv, budget, D, dtype=v.dtype, device=v.device)
+    made_k = made_v = None
+    with _memory_of(stream):
+        if k_out is None:
+            k_out = made_k = torch.empty(B, Hkv, budget, D, dtype=k.dtype, device=k.device)
+        if v_out is None:
+            v_out = made_v = torch.empty(B, Hkv, budget, D, dtype=v.dtype, device=v.device)
     st = load().kvcrush_compact(B, Hkv, S, D, _dtype_code(k), budget, _ptr(k), _ptr(v), _ptr(idx),
                                 _ptr(block_table), block_size, _ptr(_dev(k_out, "k_out")),
                                 _ptr(_dev(v_out, "v_out")), _stream(stream))
+    _hand_over(stream, made_k, made_v)
     _check(st, "kvcrush_compact")
     return k_out, v_out
 
@@ -378,8 +411,9 @@ def kvcrush_scores_append(q_new, k_cache, scores_cache, S: int, reduce_groups: b
         raise ValueError("scores_cache must be [B,Hs,capacity]")
     shape = Shape(B, Hq, Hkv, int(S), D, _dtype_code(q_new), int(bool(reduce_groups)), 0, float(scale))
     if workspace is None:
-        workspace = torch.empty(max(kvcrush_scores_append_workspace(shape, cap), 16), dtype=torch.uint8,
-                                device=q_new.device)
+        with _memory_of(stream):
+            workspace = torch.empty(max(kvcrush_scores_append_workspace(shape, cap), 16), dtype=torch.uint8,
+                                    device=q_new.device)
     if lengths is not None:
         lengths = _dev(lengths, "lengths")
         if lengths.dtype != torch.int32 or tuple(lengths.shape) != (B,):
@@ -448,10 +482,13 @@ def kvcrush_compact_block_table(idx, block_table, block_size: int, out=None, str
     if idx.dtype != torch.int32 or block_table.dtype != torch.int32 or idx.shape[0] != block_table.shape[0]:
         raise ValueError("idx and block_table must be int32 with the same batch size")
     B, budget = idx.shape
+    made = None
     if out is None:
-        out = torch.empty(B, budget // block_size, dtype=torch.int32, device=idx.device)
+        with _memory_of(stream):
+            out = made = torch.empty(B, budget // block_size, dtype=torch.int32, device=idx.device)
     st = load().kvcrush_compact_block_table(B, block_table.shape[1] * block_size, budget, block_size, _ptr(idx),
                                             _ptr(block_table), _ptr(_dev(out, "out")), _stream(stream))
+    _hand_over(stream, made)
     _check(st, "kvcrush_compact_block_table")
     return out
 
@@ -580,14 +617,6 @@ def _stream_of(cache, stream):
     return _current_raw_stream(cache.index) if stream is None else stream.cuda_stream
 
 
-def _hand_over(stream, *made):
-    """Tensors made under the current stream for a call that uses them on `stream`."""
-    if stream is not None:
-        for t in made:
-            if t is not None:
-                t.record_stream(stream)
-
-
 def kvcrush_cache_write(cache: Cache, k_new, v_new, n_new=None, stream=None):
     """k_new, v_new [B,Hkv,T,D] (any strides but three zeros, D contiguous) become the last T tokens of their sequences: the cache's
     lengths count them already.  n_new int32 [B]: only the first n_new[b] of sequence b's are real.  Quantised caches
@@ -620,12 +649,11 @@ def kvcrush_cache_read(cache: Cache, idx=None, n=None, dtype=None, k_out=None, v
     if k_out is None or v_out is None:
         # (some rows may stay unwritten: those of sequences shorter than n, of empty ones)
         new = torch.zeros if cache.lengths or (cache.S < n if idx is None else cache.S == 0) else torch.empty
-        if k_out is None:
-            k_out = made_k = new(shape, dtype=dtype, device=cache.device)
-        if v_out is None:
-            v_out = made_v = new(shape, dtype=dtype, device=cache.device)
-        if stream is not None and new is torch.zeros:   # (the zeros are written under the current stream)
-            stream.wait_stream(torch.cuda.current_stream(cache.device))
+        with _memory_of(stream):
+            if k_out is None:
+                k_out = made_k = new(shape, dtype=dtype, device=cache.device)
+            if v_out is None:
+                v_out = made_v = new(shape, dtype=dtype, device=cache.device)
     k_at, v_at = _packed(k_out, "k_out", index, dtype, shape), _packed(v_out, "v_out", index, dtype, shape)
     with _Device(index):
         st = load().kvcrush_cache_read(cache, n, at, _dtype_code(k_out), k_at, v_at, _stream_of(cache, stream))
@@ -674,29 +702,30 @@ def kvcrush_attend(cache: Cache, q, mask=None, n_new=None, blocks=None, unit=0, 
         args.n_list, args.unit = blocks.shape[-1], unit
     if n_new is not None:
         args.n_new = _counts(n_new, cache)
-    made_out = made_lse = made_ws = None
-    if out is None:
-        out = made_out = torch.empty(shape, dtype=q.dtype, device=cache.device)
-    else:
+    made_out = made_lse = None
+    if out is not None:
         _rows(out, "out", index)
         if out.shape != shape or out.dtype != q.dtype:
             raise ValueError("out must have q's shape and type")
         st = _strides(out)
         if st is not None:
             args.out_stride = st
-    if lse is None:
-        lse = made_lse = torch.empty(shape[:3], dtype=torch.float32, device=cache.device)
-    else:
+    if lse is not None:
         _packed(lse, "lse", index, torch.float32, shape[:3])
-    L = load()
-    if workspace is None:
-        workspace = made_ws = torch.empty(max(L.kvcrush_attend_workspace(cache, args), 16), dtype=torch.uint8, device=cache.device)
-    else:
+    if workspace is not None:
         _scratch(workspace, index)
+    L = load()
+    with _memory_of(stream):
+        if out is None:
+            out = made_out = torch.empty(shape, dtype=q.dtype, device=cache.device)
+        if lse is None:
+            lse = made_lse = torch.empty(shape[:3], dtype=torch.float32, device=cache.device)
+        if workspace is None:
+            workspace = torch.empty(max(L.kvcrush_attend_workspace(cache, args), 16), dtype=torch.uint8, device=cache.device)
     with _Device(index):
         st = L.kvcrush_attend(cache, args, q.data_ptr(), out.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                               _stream_of(cache, stream))
-    _hand_over(stream, made_out, made_lse, made_ws)
+    _hand_over(stream, made_out, made_lse)
     _check(st, "kvcrush_attend")
     return out, lse
 
@@ -718,10 +747,9 @@ def kvcrush_block_bounds(cache: Cache, unit: int, bounds=None, scales=None, T=0,
         raise ValueError("bounds and scales come together, and are needed to refresh blocks of them")
     made = (None, None)
     if bounds is None:
-        made = bounds, scales = (torch.zeros(of_bounds, dtype=torch.int8, device=cache.device),
-                                 torch.zeros(of_scales, dtype=torch.float32, device=cache.device))
-        if stream is not None:
-            stream.wait_stream(torch.cuda.current_stream(cache.device))
+        with _memory_of(stream):
+            made = bounds, scales = (torch.zeros(of_bounds, dtype=torch.int8, device=cache.device),
+                                     torch.zeros(of_scales, dtype=torch.float32, device=cache.device))
     bounds_at = _packed(bounds, "bounds", index, torch.int8, of_bounds)
     scales_at = _packed(scales, "scales", index, torch.float32, of_scales)
     with _Device(index):
@@ -746,21 +774,22 @@ def kvcrush_block_select(cache: Cache, q, bounds, scales, unit: int, n_select: i
     scales_at = _packed(scales, "scales", index, torch.float32, of_scales)
     if n_new is not None:
         args.n_new = _counts(n_new, cache)
-    L, made_blocks, made_ws = load(), None, None
+    L, made = load(), None
     shape = (cache.B, cache.Hkv, q.shape[2], n_select)
-    if blocks is None:
-        blocks = made_blocks = torch.empty(shape if n_select > 0 else 0, dtype=torch.int32, device=cache.device)
-    else:
+    if blocks is not None:
         _packed(blocks, "blocks", index, torch.int32, shape)
-    if workspace is None:
-        need = L.kvcrush_block_select_workspace(cache, args, unit, n_select)
-        workspace = made_ws = torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
-    else:
+    if workspace is not None:
         _scratch(workspace, index)
+    with _memory_of(stream):
+        if blocks is None:
+            blocks = made = torch.empty(shape if n_select > 0 else 0, dtype=torch.int32, device=cache.device)
+        if workspace is None:
+            need = L.kvcrush_block_select_workspace(cache, args, unit, n_select)
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
     with _Device(index):
         st = L.kvcrush_block_select(cache, args, unit, n_select, n_sink, n_recent, q.data_ptr(), bounds_at, scales_at,
                                     blocks.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_of(cache, stream))
-    _hand_over(stream, made_blocks, made_ws)
+    _hand_over(stream, made)
     _check(st, "kvcrush_block_select")
     return blocks
 

@@ -92,3 +92,50 @@ def test_scratch_memory_does_not_pile_up():
         for n_select in (0, 8):
             cache.attend(torch.zeros(1, 32, T, 128, dtype=torch.bfloat16, device="cuda"), n_select=n_select)
     assert torch.cuda.memory_allocated() == before
+
+
+@pytest.mark.gpu
+def test_what_a_call_on_another_stream_makes_is_not_in_use():
+    """Work is pending on the current stream that still writes tensors which are free already; results and scratch memory of
+    calls on another stream, whose sizes fit, must not be there."""
+    B, Hq, Hkv, S, D = 2, 8, 2, 1024, 128
+    q, k, v = (values((B, H, S, D), i).cuda() for i, H in enumerate((Hq, Hkv, Hkv)))
+    new, scores0 = q[:, :, -1].contiguous(), torch.rand(B, Hkv, S, device="cuda")
+    table = torch.arange(B * S // 16, dtype=torch.int32, device="cuda").view(B, -1)
+    cache = kv.make_cache(k, v, S)
+    bnd = kv.kvcrush_block_bounds(cache, 16)
+    idx, *_ = kv.kvcrush_select(scores0, 512, 256, unit=16)
+
+    def calls(stream, running):
+        scores, _ = kv.kvcrush_scores(q, k, True, stream=stream)
+        yield scores
+        yield kv.kvcrush_row_lse(q, k, stream=stream)
+        yield kv.kvcrush_pool_scores(scores0, 7, stream=stream)
+        yield from kv.kvcrush_select(scores0, 512, 256, want_bits=True, stream=stream)
+        yield from kv.kvcrush_compact(k, v, idx, validate=False, stream=stream)
+        yield kv.kvcrush_compact_block_table(idx, table, 16, stream=stream)
+        yield kv.kvcrush_scores_append(new, k, running, S, True, stream=stream)
+        yield from kv.kvcrush_cache_read(cache, stream=stream)
+        yield from kv.kvcrush_cache_read(cache, idx=idx, stream=stream)
+        yield from kv.kvcrush_block_bounds(cache, 16, stream=stream)
+        blocks = kv.kvcrush_block_select(cache, q[:, :, -4:], *bnd, 16, 20, stream=stream)
+        yield blocks
+        yield from kv.kvcrush_attend(cache, q[:, :, -4:], stream=stream)
+        yield from kv.kvcrush_attend(cache, q[:, :, -4:], blocks=blocks, unit=16, stream=stream)
+
+    want = [x.clone() for x in calls(None, scores0.clone())]
+    torch.cuda.synchronize()
+    running, side, a = scores0.clone(), torch.cuda.Stream(), torch.randn(8192, 8192, device="cuda", dtype=torch.bfloat16)
+    a @ a
+    torch.cuda.synchronize()
+    sizes = sorted({x.nbytes for x in want} | {16 << i for i in range(21)})
+    filled = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]
+    for _ in range(20):                                        # some 20 ms
+        a @ a
+    for x in filled:
+        x.fill_(0xAB)
+    filled = x = None
+    got = list(calls(side, running))
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
