@@ -11,6 +11,7 @@ import ctypes
 import os
 
 import torch
+from torch.autograd import forward_ad
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libkvcrush.so")
@@ -534,11 +535,31 @@ def make_cache(k, v, S: int, k_param=None, v_param=None, lengths=None, block_tab
         raise ValueError("the cache's tensors must live on one device")
     if any(t is not None and t.requires_grad for t in tensors):
         raise ValueError("the cache's tensors must not require gradients: the calls on it have none")
+    for name, t in zip(("k", "v", "k_param", "v_param"), tensors):
+        if t is not None:
+            _untracked(t, name)
     cache = Cache(B, Hkv, int(S), D, capacity, fmt, block_size, n_blocks, *(None if t is None else t.data_ptr() for t in tensors))
     cache.tensors, cache.device, cache.index = tensors, k.device, k.get_device()
     cache.value_dtype = torch.bfloat16 if k.dtype in CODES.values() else k.dtype
-    cache.per_sequence = (B,)
+    cache.per_sequence, cache.values = (B,), (k_param, v_param) if fmt in (E4M3, I8, I4) else (k, v)
     return cache
+
+
+def _untracked(t, name: str):
+    """Autograd does not follow t, in neither direction: the calls on a cache would cut it off without a word."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, and the calls on a cache have none: use torch.no_grad() or detach()")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} has a forward-mode tangent, and the calls on a cache carry none on: use its primal part")
+
+
+def _untracked_cache(cache):
+    """Its tensors may have come to be followed since make_cache, by what was copied into them."""
+    a, b = cache.values
+    if a.requires_grad or b.requires_grad or forward_ad._current_level >= 0:
+        for t in (a, b):
+            if t.grad_fn is not None or not t.requires_grad:
+                _untracked(t, "the cache")
 
 
 def _here(t, name: str, index: int):
@@ -553,6 +574,8 @@ def _packed(t, name: str, index: int, dtype, shape):
         raise ValueError(f"{name} must be {dtype} {list(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _untracked(t, name)
     return t.data_ptr()
 
 
@@ -567,8 +590,8 @@ def _rows(t, name: str, index: int):
     _here(t, name, index)
     if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
         raise ValueError(f"{name} must be [B,H,T,D] with the D values contiguous")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} requires a gradient, and the calls on a cache have none: use torch.no_grad() or detach()")
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _untracked(t, name)
 
 
 def _strides(t):
@@ -622,6 +645,7 @@ def kvcrush_cache_write(cache: Cache, k_new, v_new, n_new=None, stream=None):
     lengths count them already.  n_new int32 [B]: only the first n_new[b] of sequence b's are real.  Quantised caches
     take float32, bfloat16 and float16, the others their own type."""
     index, shape = cache.index, k_new.shape
+    _untracked_cache(cache)
     _rows(k_new, "k_new", index), _rows(v_new, "v_new", index)
     if v_new.shape != shape or v_new.dtype != k_new.dtype or shape[0] != cache.B or shape[1] != cache.Hkv or shape[3] != cache.D:
         raise ValueError("k_new and v_new must be [B,Hkv,T,D] tensors of one type that fit the cache")
@@ -637,6 +661,7 @@ def kvcrush_cache_read(cache: Cache, idx=None, n=None, dtype=None, k_out=None, v
     -> (k, v) [B,Hkv,n,D] of `dtype` (default: k_out's; the cache's own type; bfloat16 of quantised ones).  Rows that a
     sequence does not have stay as they are in k_out and v_out; in tensors made here they are zero."""
     index, at = cache.index, None
+    _untracked_cache(cache)
     if idx is not None:
         n = idx.shape[-1]
         at = _packed(idx, "idx", index, torch.int32, (cache.B, n))
@@ -670,6 +695,7 @@ def kvcrush_attend_workspace(cache: Cache, Hq: int, T: int, dtype, n_list=0, uni
 
 
 def _queries(cache, q):
+    _untracked_cache(cache)
     _rows(q, "q", cache.index)
     B, Hq, T, D = q.shape
     dtype = q.dtype
@@ -742,6 +768,7 @@ def kvcrush_block_bounds(cache: Cache, unit: int, bounds=None, scales=None, T=0,
     Nb = ceil(capacity / unit).  T > 0 refreshes, in bounds and scales given, the blocks of the last T tokens (of the
     n_new[b] real ones) only."""
     index = cache.index
+    _untracked_cache(cache)
     of_bounds, of_scales = _block_shapes(cache, unit)
     if (bounds is None) != (scales is None) or (bounds is None and T):
         raise ValueError("bounds and scales come together, and are needed to refresh blocks of them")

@@ -139,3 +139,38 @@ def test_what_a_call_on_another_stream_makes_is_not_in_use():
     torch.cuda.synchronize()
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+
+
+@pytest.mark.gpu
+def test_what_autograd_follows_is_refused_in_both_directions():
+    """Tangents, outputs that require a gradient, a cache that came to be followed by what was copied into it."""
+    from torch.autograd import forward_ad
+    c = kv_cache(None, B=1, n=40, capacity=64)
+    q, k = values((1, 4, 1, 128), 1).cuda(), values((1, 2, 1, 128), 2).cuda()
+    lse, rows = torch.empty(1, 4, 1, device="cuda"), torch.empty(1, 2, 40, 128, dtype=torch.bfloat16, device="cuda")
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: c.attend(dual(q)), lambda: c.attend(dual(q), n_select=2), lambda: c.append(dual(k), k),
+                     lambda: c.append(k, dual(k)), lambda: kv.kvcrush_attend(c.cache, q, lse=dual(lse)),
+                     lambda: kv.kvcrush_attend(c.cache, q, out=dual(q)), lambda: kv.make_cache(dual(c.k), c.v, 40),
+                     lambda: kv.kvcrush_cache_read(c.cache, n=40, k_out=dual(rows)), lambda: kv.make_cache(c.k, dual(c.v), 40)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        assert c.lengths.tolist() == [40] and c.bound == 40
+        c.attend(q)                                            # (nothing is dual: as ever)
+    for call in (lambda: kv.kvcrush_attend(c.cache, q, lse=lse.requires_grad_()),
+                 lambda: kv.kvcrush_cache_read(c.cache, n=40, v_out=rows.requires_grad_()),
+                 lambda: kv.kvcrush_block_bounds(c.cache, 16, c.bounds, c.bound_scales.detach().requires_grad_())):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    d = decode_cache()
+    d.attend(values((1, 4, 64), 1).cuda())
+    with torch.no_grad():
+        d.append(values((1, 4, 64), 1).cuda(), *(values((1, 2, 64), 2).cuda().requires_grad_() for _ in range(2)))
+        d.attend(values((1, 4, 64), 1).cuda())
+    d.append(values((1, 4, 64), 1).cuda(), *(values((1, 2, 64), 2).cuda().requires_grad_() for _ in range(2)))
+    with pytest.raises(ValueError, match="gradient"):
+        d.attend(values((1, 4, 64), 1).cuda())
+    with torch.no_grad():
+        out, _ = d.attend(values((1, 4, 64), 1).cuda())
+    assert torch.isfinite(out).all()
