@@ -229,11 +229,13 @@ class KVCache:
                      doc="No sequence is longer than this: the calls read up to it, whatever `lengths` says.")
 
     def append(self, k_new, v_new, n_new=None):
-        """k_new, v_new [B,Hkv,T,D]: T tokens more for every sequence, or the first n_new[b] (int32 [B] on the GPU, 0 to T)
-        of them.  A sequence must not outgrow the capacity (the caller's to see to where n_new decides)."""
+        """k_new, v_new [B,Hkv,T,D]: T tokens more for every sequence, or the first n_new[b] (int32 [B] on the GPU, 0 to T;
+        pulled into that range) of them.  A sequence must not outgrow the capacity (the caller's to see to where n_new
+        decides)."""
         T = k_new.shape[2]
         if n_new is None and self.bound + T > self.capacity:
             raise ValueError(f"{T} tokens more may pass the capacity of {self.capacity}: set `bound` to the longest length")
+        n_new = None if n_new is None else n_new.clamp(0, T)
         self.lengths.add_(T if n_new is None else n_new)
         before, self.bound = self.bound, min(self.bound + T, self.capacity)
         try:
@@ -248,11 +250,11 @@ class KVCache:
             raise
 
     def drop(self, n):
-        """The last n tokens (a number, or int32 [B] on the GPU, not negative) of every sequence are taken back, as rejected
-        drafts are; a sequence that has fewer is empty then."""
+        """The last n tokens (a number, not negative, or int32 [B] on the GPU, where a negative one counts as 0) of every
+        sequence are taken back, as rejected drafts are; a sequence that has fewer is empty then."""
         if isinstance(n, int) and n < 0:
             raise ValueError("n must not be negative")
-        self.lengths.sub_(n).clamp_(min=0)
+        self.lengths.sub_(n if isinstance(n, int) else n.clamp(min=0)).clamp_(min=0)
         if isinstance(n, int):
             self.bound = max(self.bound - n, 0)
 

@@ -174,3 +174,26 @@ def test_what_autograd_follows_is_refused_in_both_directions():
     with torch.no_grad():
         out, _ = d.attend(values((1, 4, 64), 1).cuda())
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [None, "i8"])
+def test_counts_outside_their_range_count_as_its_ends(fmt):
+    """More tokens than were given are as many as were given, less than none are none: lengths never pass what is written."""
+    made = [kv_cache(fmt, B=3, n=20, capacity=64, unit=8) for _ in range(2)]
+    k = values((3, 2, 4, 128), 9).cuda()
+    counts = lambda *n: torch.tensor(n, dtype=torch.int32, device="cuda")  # noqa: E731
+    for step in range(2):
+        made[0].append(k, k, n_new=counts(7 + step, -3, 2 ** 31 - 1 - step))
+        made[1].append(k, k, n_new=counts(4, 0, 4))
+    given = counts(2, -5, -2 ** 31)
+    made[0].drop(given)
+    made[1].drop(counts(2, 0, 0))
+    assert given.tolist() == [2, -5, -2 ** 31] and made[0].lengths.tolist() == made[1].lengths.tolist() == [26, 20, 28]
+    q = values((3, 4, 1, 128), 3).cuda()
+    for n_select in (0, 2):
+        for x, y in zip(*(c.attend(q, n_select=n_select) for c in made)):
+            assert torch.equal(x, y)
+    with pytest.raises(ValueError):                            # a refused append takes back what it counted, no more
+        made[0].append(k, k[:, :1], n_new=counts(9, -9, 1))
+    assert made[0].lengths.tolist() == [26, 20, 28]
