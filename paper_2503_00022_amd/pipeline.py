@@ -257,6 +257,8 @@ class KVCache:
         self.lengths.sub_(n if isinstance(n, int) else n.clamp(min=0)).clamp_(min=0)
         if isinstance(n, int):
             self.bound = max(self.bound - n, 0)
+        if self.unit:   # (the last block's bounds without what it has no more; later blocks are nobody's)
+            kv.kvcrush_block_bounds(self.cache, self.unit, self.bounds, self.bound_scales, T=1)
 
     def attend(self, q, mask=None, n_new=None, n_select=0, n_sink=1, n_recent=1):
         """The last T tokens attend to the cache: q [B,Hq,T,D], mask and n_new as kvcrush_attend takes them -> (out, lse).

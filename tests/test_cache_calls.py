@@ -197,3 +197,24 @@ def test_counts_outside_their_range_count_as_its_ends(fmt):
     with pytest.raises(ValueError):                            # a refused append takes back what it counted, no more
         made[0].append(k, k[:, :1], n_new=counts(9, -9, 1))
     assert made[0].lengths.tolist() == [26, 20, 28]
+
+
+@pytest.mark.gpu
+def test_a_drop_refreshes_the_bounds_of_the_last_block():
+    """Taken back tokens have no say in which blocks are chosen, also before the next append."""
+    B, Hkv, D, unit = 2, 2, 64, 8
+    made = [KVCache(B, Hkv, 128, D, unit=unit) for _ in range(2)]
+    k = values((B, Hkv, 60, D), 1).cuda()
+    k[:, :, 43:] *= 50                                         # (blocks 5 to 7: what is dropped would win every choice)
+    for c, n in zip(made, (60, 43)):
+        c.append(k[:, :, :n], k[:, :, :n])
+    made[0].drop(10)
+    made[0].drop(torch.tensor([7, 7], dtype=torch.int32, device="cuda"))
+    live = -(-43 // unit)
+    assert torch.equal(made[0].bounds[:, :, :live], made[1].bounds[:, :, :live])
+    assert torch.equal(made[0].bound_scales[:, :, :live], made[1].bound_scales[:, :, :live])
+    q = values((B, 4, 1, D), 3).cuda()
+    for x, y in zip(*(c.attend(q, n_select=2, n_sink=0, n_recent=0) for c in made)):
+        assert torch.equal(x, y)
+    made[0].drop(100)                                          # (nothing is left: no block to refresh)
+    assert made[0].lengths.tolist() == [0, 0]
