@@ -186,7 +186,7 @@ class KVCache:
     tree of drafted ones, over all of it or over the blocks that suit each query.
 
     B sequences of up to `capacity` tokens.  `format`: None keeps rows in `dtype`; "e4m3", "i8" and "i4" quantise them as
-    they are written.  `block_size` > 0: paged, with `block_table` int32 [B, capacity / block_size] into a pool of
+    they are written (`dtype`, bfloat16 or float16, is then that of the queries, the results and of what read() gives).  `block_size` > 0: paged, with `block_table` int32 [B, capacity / block_size] into a pool of
     `n_blocks` (without one, sequence b owns blocks b * capacity / block_size and following).  `unit` > 0 keeps bounds of
     blocks of that many tokens, which attend(n_select=..) chooses by.
     lengths (int32 [B] on the GPU) counts each sequence's tokens; nothing here synchronises.  The calls capture into a HIP
@@ -202,6 +202,16 @@ class KVCache:
             raise ValueError("capacity must be a multiple of block_size")
         if block_table is not None and not block_size:
             raise ValueError("a block_table needs a block_size")
+        if block_table is not None and (tuple(block_table.shape) != (B, capacity // block_size) or n_blocks < 1):
+            raise ValueError("a block_table must be [B, capacity / block_size] and needs the pool's n_blocks")
+        # (what no call on such a cache would take is refused before it holds anything)
+        if D not in (64, 128):
+            raise ValueError("D must be 64 or 128")
+        if format is not None and dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("a quantised cache is attended to in bfloat16 or float16: dtype must be one of them (append takes "
+                             "float32 rows, read gives them)")
+        if unit < 0 or unit > 1024:
+            raise ValueError("unit must be 1 to 1024 tokens, or 0")
         dev = torch.device(device)
         if block_size:
             per = capacity // block_size

@@ -218,3 +218,23 @@ def test_a_drop_refreshes_the_bounds_of_the_last_block():
         assert torch.equal(x, y)
     made[0].drop(100)                                          # (nothing is left: no block to refresh)
     assert made[0].lengths.tolist() == [0, 0]
+
+
+def test_caches_that_no_call_would_take_are_refused_at_once():
+    """Before anything is allocated: no GPU is needed."""
+    table = torch.zeros(1, 2, dtype=torch.int32)
+    for change, match in ((dict(D=96), "64 or 128"), (dict(format="i8", dtype=torch.float32), "bfloat16 or float16"),
+                          (dict(unit=1025), "unit"), (dict(unit=-1), "unit"), (dict(block_size=16, block_table=table), "n_blocks"),
+                          (dict(block_size=8, block_table=table, n_blocks=9), "block_table")):
+        with pytest.raises(ValueError, match=match):
+            KVCache(1, 1, 32, **dict(dict(D=64, device="cpu"), **change))
+
+
+@pytest.mark.gpu
+def test_single_precision_rows_of_a_quantised_cache():
+    c = KVCache(1, 2, 32, 64, format="i8")
+    k = values((1, 2, 20, 64), 1, torch.float32).cuda()
+    c.append(k, k)
+    codes, par = ref.quantise(k.cpu().numpy(), "i8")
+    assert torch.equal(c.read(dtype=torch.float32)[0].cpu(), torch.from_numpy(ref.values32(codes, par, "i8")))
+    assert c.attend(values((1, 4, 1, 64), 2).cuda())[0].dtype == torch.bfloat16
