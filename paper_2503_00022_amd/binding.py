@@ -724,6 +724,8 @@ def kvcrush_attend(cache: Cache, q, mask=None, n_new=None, blocks=None, unit=0, 
         args.mask = _packed(mask, "mask", index, torch.int64, (B, T, words) if mask.dim() == 3 else (T, words))
         args.mask_stride = T * words if mask.dim() == 3 else 0
     if blocks is not None:
+        if blocks.shape[-1] < 1:   # (no entries have no address, which is the library's sign for all tokens)
+            raise ValueError("blocks must have one entry a list at least")
         args.blocks = _packed(blocks, "blocks", index, torch.int32, (B, cache.Hkv, T, blocks.shape[-1]))
         args.n_list, args.unit = blocks.shape[-1], unit
     if n_new is not None:

@@ -238,3 +238,13 @@ def test_single_precision_rows_of_a_quantised_cache():
     codes, par = ref.quantise(k.cpu().numpy(), "i8")
     assert torch.equal(c.read(dtype=torch.float32)[0].cpu(), torch.from_numpy(ref.values32(codes, par, "i8")))
     assert c.attend(values((1, 4, 1, 64), 2).cuda())[0].dtype == torch.bfloat16
+
+
+@pytest.mark.gpu
+def test_lists_without_entries_are_refused():
+    c = kv_cache(None, n=40, capacity=64)
+    q = values((2, 4, 1, 128), 1).cuda()
+    with pytest.raises(ValueError, match="one entry"):
+        kv.kvcrush_attend(c.cache, q, blocks=torch.empty(2, 2, 1, 0, dtype=torch.int32, device="cuda"), unit=16)
+    out, lse = kv.kvcrush_attend(c.cache, q, blocks=torch.full((2, 2, 1, 1), -1, dtype=torch.int32, device="cuda"), unit=16)
+    assert not out.any() and (lse == -float("inf")).all()
