@@ -46,7 +46,7 @@ def build_library(verbose: bool = False, extra_flags=()) -> str:
     with tempfile.TemporaryDirectory() as folder, ThreadPoolExecutor(max(1, min(len(os.sched_getaffinity(0)), 16))) as pool:
         jobs = [pool.submit(compile_one, src, os.path.join(folder, os.path.basename(src) + ".o")) for src in sources()]
         objects = [j.result() for j in jobs]
-        subprocess.run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects], check=True)
+        subprocess.run([hipcc, *HIPCC_FLAGS, *extra_flags, "-o", tmp, *objects], check=True)
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 

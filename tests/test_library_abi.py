@@ -437,3 +437,19 @@ def test_score_loops_wait_only_where_they_must(tmp_path):
         assert "global_load_lds_dwordx4" in loop
         checked += 1
     assert checked == 16, checked   # {lse, colsum} x {bf16, fp16} x {D = 64, 128} x {packed, strided}
+
+
+def test_extra_flags_reach_the_compiler_and_the_linker(tmp_path, monkeypatch):
+    """build_library(extra_flags=..): every source is compiled with them, and the library is linked with them."""
+    from paper_2503_00022_amd import build
+    log, fake = tmp_path / "log", tmp_path / "hipcc"
+    fake.write_text('#!/bin/sh\necho "$@" >> %s\nwhile [ "$1" != "-o" ]; do shift; done\n: > "$2"\n' % log)
+    fake.chmod(0o755)
+    monkeypatch.setenv("HIPCC", str(fake))
+    monkeypatch.setattr(build, "LIB_PATH", str(tmp_path / "lib.so"))
+    assert build.build_library(extra_flags=("-g", "-Wl,--build-id")) == str(tmp_path / "lib.so")
+    calls = log.read_text().splitlines()
+    assert len(calls) == len(build.sources()) + 1
+    for call in calls:
+        assert "-g -Wl,--build-id" in call and "--offload-arch=gfx950" in call and "-O3" in call
+    assert sum("-shared" in call for call in calls) == 1 and "-shared" in calls[-1]
