@@ -230,6 +230,7 @@ class KVCache:
         self.lengths, self.block_table = new(B, dtype=torch.int32), block_table
         self.capacity, self.dtype, self.unit, self.scale = capacity, dtype, unit, scale
         self.cache = kv.make_cache(self.k, self.v, 0, self.k_param, self.v_param, self.lengths, block_table)
+        self._written = (self.k, self.v) if format is None else (self.k, self.v, self.k_param, self.v_param)
         self.bounds = self.bound_scales = None
         if unit:
             nb = (capacity + unit - 1) // unit
@@ -251,7 +252,7 @@ class KVCache:
         try:
             kv.kvcrush_cache_write(self.cache, k_new, v_new, n_new=n_new)
             if not self.k.is_inference():
-                increment_version((self.k, self.v))  # (a backward pass that saved the cache is to notice)
+                increment_version(self._written)  # (a backward pass that saved the cache is to notice)
             if self.unit:
                 kv.kvcrush_block_bounds(self.cache, self.unit, self.bounds, self.bound_scales, T=T, n_new=n_new)
         except Exception:   # (a refused call leaves the cache as long as it was)

@@ -248,3 +248,16 @@ def test_lists_without_entries_are_refused():
         kv.kvcrush_attend(c.cache, q, blocks=torch.empty(2, 2, 1, 0, dtype=torch.int32, device="cuda"), unit=16)
     out, lse = kv.kvcrush_attend(c.cache, q, blocks=torch.full((2, 2, 1, 1), -1, dtype=torch.int32, device="cuda"), unit=16)
     assert not out.any() and (lse == -float("inf")).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["k_param", "v_param"])
+def test_a_backward_pass_notices_an_append_to_a_quantised_cache(name):
+    c = KVCache(1, 2, 16, 64, format="i8")
+    x = values((1, 2, 3, 64), 1).cuda()
+    c.append(x, x)
+    t = getattr(c, name)
+    y = (torch.ones_like(t, requires_grad=True) * t).sum()
+    c.append(x, x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()

@@ -171,3 +171,15 @@ def test_rows_without_a_range(rows, level):
     c = made("i4", k, v)
     q = torch.ones(1, Hq, T, D).bfloat16()
     check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [T])
+
+
+@pytest.mark.parametrize("fmt", ref.FORMATS)
+@pytest.mark.parametrize("T,lengths,Hq,Hkv,kind", [(1024, [1100], 2, 1, "tree"), (300, [300, 900], 4, 2, "chain"), (513, [800], 3, 3, "tree")])
+def test_many_new_tokens(fmt, T, lengths, Hq, Hkv, kind):
+    """Up to as many as a call takes: masks of several words, tiles of nothing but new tokens."""
+    B, D = len(lengths), 64
+    c = ref.Case(fmt, B, Hkv, lengths, D, block_size=16, seed=T).cuda()
+    q, rng = values((B, Hq, T, D), q_type(fmt), 4), np.random.RandomState(T)
+    seen = np.stack([ref.tree(T, rng) for _ in range(B)]) if kind == "tree" else None
+    got = kv.kvcrush_attend(c.make(kv), q.cuda(), mask=None if seen is None else ref.mask_words(seen).cuda())
+    check_attention(c, q, got, [min(T, n) for n in lengths], seen)
