@@ -183,3 +183,33 @@ def test_many_new_tokens(fmt, T, lengths, Hq, Hkv, kind):
     seen = np.stack([ref.tree(T, rng) for _ in range(B)]) if kind == "tree" else None
     got = kv.kvcrush_attend(c.make(kv), q.cuda(), mask=None if seen is None else ref.mask_words(seen).cuda())
     check_attention(c, q, got, [min(T, n) for n in lengths], seen)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f16", "f32", "e4m3", "i8", "i4"])
+@pytest.mark.parametrize("Hq,Hkv,T", [(8, 2, 3), (40, 2, 1)])
+def test_infinities_in_chosen_and_other_blocks(fmt, Hq, Hkv, T):
+    """Lists of blocks, lengths and counts on the device: the first token, in no list, is NaN; a chosen block holds an infinity
+    (quantised: a row of NaN), which those rows that have it in their list see."""
+    B, D, unit, lengths = 2, 64, 8, [300, 77]
+    rng = np.random.RandomState(5)
+    k, v = (rng.randn(B, Hkv, 300, D).astype(np.float32) for _ in range(2))
+    v[:, :, 0] = math.nan
+    v[:, 0, 3 * unit + 2, 5] = math.inf
+    c = made(fmt, k, v, 16)
+    c.lengths = lengths
+    lists = [[[[3, 5, 9] if t % 2 else [2, 4, 7] for t in range(T)] if g == 0 else [[1, 6, 8]] * T for g in range(Hkv)] for _ in range(B)]
+    q = values((B, Hq, T, D), q_type(fmt), 9)
+    n_new = [T, max(T - 1, 1)]
+    cache = c.make(kv)
+    got = kv.kvcrush_attend(cache, q.cuda(), blocks=torch.tensor(lists, dtype=torch.int32).cuda(), unit=unit,
+                            n_new=torch.tensor(n_new, dtype=torch.int32, device="cuda"))
+    c.rows64["v"] = np.where(np.isfinite(c.rows64["v"]), c.rows64["v"], 0.0)
+    out = got[0].cpu().double().numpy()
+    want = ref.attend(q.double().numpy(), c.rows64["k"], c.rows64["v"], lengths, n_new, None, None, lists, unit)[0]
+    for b in range(B):
+        for t in range(1, n_new[b], 2):                        # (those that have block 3)
+            hit = out[b, :Hq // Hkv, t]
+            assert (hit[:, 5] == math.inf).all() if fmt in ref.DTYPES else np.isnan(hit).all()
+            at = 5 if fmt in ref.DTYPES else slice(None)
+            out[b, :Hq // Hkv, t, at] = want[b, :Hq // Hkv, t, at]
+    check_attention(c, q, (torch.from_numpy(out), got[1]), n_new, lists=lists, unit=unit)
