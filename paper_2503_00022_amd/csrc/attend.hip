@@ -13,13 +13,12 @@
 // end the workgroup's waves add up their rows.  The keys of a sequence are cut over workgroups so that the chip is
 // full; the pieces' results are merged by a second kernel.
 //
-// Measured: 8 sequences of 2048 bf16 keys, 67 MB, 17 us (4.0 TB/s; 22 where they come from memory and not from the
-// last-level cache) and 4 to merge; 4 paged e4m3 caches of up to 32768 keys, 225 MB, 55 to 58 us (4.1 TB/s; 3 to 8 of them
-// until the first tiles are there); 64 rows over 16384 bf16 keys 25 us, of which a tile of 32 keys takes 2.5 on eight waves
-// and the first one, with the code still to be fetched, 5; 256 rows over 2 x 7839 8-bit keys 43 us, a wave and
-// tile of 32 rows being 510 vector instructions and 48 matrix instructions: those issue in 60 % of the time, these take 20,
-// and the rest is the way through the LDS and the barriers.  (Halves of the codes made once for the four waves that share a
-// tile: a fifth fewer vector instructions, one more way through the LDS, no faster.)
+// Measured: 8 sequences of 2048 bf16 keys, 67 MB, 16 us (4.3 TB/s; more where they come from memory and not from the
+// last-level cache) and 4 to merge; 4 paged e4m3 caches of up to 32768 keys, 225 MB, 50 to 57 us (4.1 TB/s; 3 to 8 of them
+// until the first tiles are there); 64 rows over 16384 bf16 keys 23.5 us, four tiles a wave, so that the way to the first
+// tile, its code still to be fetched, and the end are half of it; 256 rows over 2 x 7839 8-bit keys 46 us, a wave and
+// tile of 32 rows being about 510 vector instructions and 48 matrix instructions: those issue in 60 % of the time, these
+// take 20, and the rest is the way through the LDS and the barriers.
 #include <algorithm>
 #include <cmath>
 
@@ -994,7 +993,7 @@ struct Plan {
 };
 
 // Keys that one workgroup reads each, and that are more than half of the last-level cache's 256 MB holds, pass the caches
-// by: nothing of them is left there for the next step.  (225 MB: 61 -> 57 us; 67 MB, which do stay: 18.6 -> 20.0.  Where
+// by: nothing of them is left there for the next step.  (225 MB: 61 -> 55 us; 67 MB, which do stay: 18.6 -> 20.0.  Where
 // row tiles or queries share keys, 6 % slower.)
 constexpr long long kOnceBytes = 128ll << 20;
 constexpr long long kUnits = 256;  // compute units of the chip

@@ -1,7 +1,8 @@
 // Which blocks of a cache a query attends to: 8-bit bounds of each block's keys, kept as the cache grows, and the
 // choice of the best blocks by them.
 //
-// A block's score for a query is sum_d max(q_d lo_d, q_d hi_d), an upper bound of its keys' products, with q, lo and
+// A block's score for a query is sum_d max(q_d lo_d, q_d hi_d), an upper bound of its keys' products (of a box around them,
+// as J. Tang et al. choose pages by in "Query-Aware Sparsity for Efficient Long-Context LLM Inference", 2024), with q, lo and
 // hi in 8 bits: an integer below 2^24, so that it is the same in whatever order it is summed, on the matrix cores as
 // 2 D products of [min(q, 0), max(q, 0)] with [lo, hi].  Choosing reads 2 D + 4 bytes per block and KV head where
 // attending to the block reads 2 unit rows.  All three kernels are latency at one token: 3.9, 5.3 and 7.0 us for 2048 blocks
