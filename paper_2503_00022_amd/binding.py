@@ -555,7 +555,7 @@ def _untracked(t, name: str):
 
 def _untracked_cache(cache):
     """Its tensors may have come to be followed since make_cache, by what was copied into them."""
-    a, b = cache.values
+    a, b = cache.values  # (set by make_cache)
     if a.requires_grad or b.requires_grad or forward_ad._current_level >= 0:
         for t in (a, b):
             if t.grad_fn is not None or not t.requires_grad:
@@ -645,8 +645,8 @@ def kvcrush_cache_write(cache: Cache, k_new, v_new, n_new=None, stream=None):
     lengths count them already.  n_new int32 [B]: only the first n_new[b] of sequence b's are real.  Quantised caches
     take float32, bfloat16 and float16, the others their own type."""
     index, shape = cache.index, k_new.shape
-    _untracked_cache(cache)
     _rows(k_new, "k_new", index), _rows(v_new, "v_new", index)
+    _untracked_cache(cache)
     if v_new.shape != shape or v_new.dtype != k_new.dtype or shape[0] != cache.B or shape[1] != cache.Hkv or shape[3] != cache.D:
         raise ValueError("k_new and v_new must be [B,Hkv,T,D] tensors of one type that fit the cache")
     with _Device(index):
@@ -661,12 +661,12 @@ def kvcrush_cache_read(cache: Cache, idx=None, n=None, dtype=None, k_out=None, v
     -> (k, v) [B,Hkv,n,D] of `dtype` (default: k_out's; the cache's own type; bfloat16 of quantised ones).  Rows that a
     sequence does not have stay as they are in k_out and v_out; in tensors made here they are zero."""
     index, at = cache.index, None
-    _untracked_cache(cache)
     if idx is not None:
         n = idx.shape[-1]
         at = _packed(idx, "idx", index, torch.int32, (cache.B, n))
     elif n is None:
         n = cache.S
+    _untracked_cache(cache)
     shape = (cache.B, cache.Hkv, n, cache.D)
     if dtype is None:
         dtype = k_out.dtype if k_out is not None else v_out.dtype if v_out is not None else cache.value_dtype
@@ -695,8 +695,8 @@ def kvcrush_attend_workspace(cache: Cache, Hq: int, T: int, dtype, n_list=0, uni
 
 
 def _queries(cache, q):
-    _untracked_cache(cache)
     _rows(q, "q", cache.index)
+    _untracked_cache(cache)
     B, Hq, T, D = q.shape
     dtype = q.dtype
     if B != cache.B or D != cache.D or dtype not in _VALUES:
@@ -770,10 +770,10 @@ def kvcrush_block_bounds(cache: Cache, unit: int, bounds=None, scales=None, T=0,
     Nb = ceil(capacity / unit).  T > 0 refreshes, in bounds and scales given, the blocks of the last T tokens (of the
     n_new[b] real ones) only."""
     index = cache.index
-    _untracked_cache(cache)
     of_bounds, of_scales = _block_shapes(cache, unit)
     if (bounds is None) != (scales is None) or (bounds is None and T):
         raise ValueError("bounds and scales come together, and are needed to refresh blocks of them")
+    _untracked_cache(cache)
     made = (None, None)
     if bounds is None:
         with _memory_of(stream):
