@@ -9,6 +9,8 @@ HIP stream; nothing synchronises.
 """
 from __future__ import annotations
 
+import operator
+
 import torch
 from torch.autograd import forward_ad
 from torch.autograd.graph import increment_version
@@ -263,10 +265,13 @@ class KVCache:
     def drop(self, n):
         """The last n tokens (a number, not negative, or int32 [B] on the GPU, where a negative one counts as 0) of every
         sequence are taken back, as rejected drafts are; a sequence that has fewer is empty then."""
-        if isinstance(n, int) and n < 0:
-            raise ValueError("n must not be negative")
-        self.lengths.sub_(n if isinstance(n, int) else n.clamp(min=0)).clamp_(min=0)
-        if isinstance(n, int):
+        if isinstance(n, torch.Tensor):
+            self.lengths.sub_(n.clamp(min=0)).clamp_(min=0)
+        else:
+            n = operator.index(n)
+            if n < 0:
+                raise ValueError("n must not be negative")
+            self.lengths.sub_(n).clamp_(min=0)
             self.bound = max(self.bound - n, 0)
         if self.unit:   # (the last block's bounds without what it has no more; later blocks are nobody's)
             kv.kvcrush_block_bounds(self.cache, self.unit, self.bounds, self.bound_scales, T=1)

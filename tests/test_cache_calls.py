@@ -261,3 +261,15 @@ def test_a_backward_pass_notices_an_append_to_a_quantised_cache(name):
     c.append(x, x)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+@pytest.mark.gpu
+def test_a_drop_takes_any_whole_number():
+    c = kv_cache(None, n=40, capacity=64)
+    c.drop(np.int64(3))
+    assert c.lengths.tolist() == [37, 37] and c.bound == 37
+    with pytest.raises(TypeError):
+        c.drop(2.5)
+    with pytest.raises(ValueError, match="negative"):
+        c.drop(np.int32(-1))
+    assert c.lengths.tolist() == [37, 37] and c.bound == 37
