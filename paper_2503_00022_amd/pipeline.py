@@ -204,8 +204,9 @@ class KVCache:
             raise ValueError("capacity must be a multiple of block_size")
         if block_table is not None and not block_size:
             raise ValueError("a block_table needs a block_size")
-        if block_table is not None and (tuple(block_table.shape) != (B, capacity // block_size) or n_blocks < 1):
-            raise ValueError("a block_table must be [B, capacity / block_size] and needs the pool's n_blocks")
+        if block_table is not None and (block_table.dim() != 2 or block_table.shape[0] != B
+                                        or block_table.shape[1] < capacity // block_size or n_blocks < 1):
+            raise ValueError("a block_table must be [B, capacity / block_size] or wider, and needs the pool's n_blocks")
         # (what no call on such a cache would take is refused before it holds anything)
         if D not in (64, 128):
             raise ValueError("D must be 64 or 128")
@@ -235,7 +236,7 @@ class KVCache:
         self._written = (self.k, self.v) if format is None else (self.k, self.v, self.k_param, self.v_param)
         self.bounds = self.bound_scales = None
         if unit:
-            nb = (capacity + unit - 1) // unit
+            nb = (self.cache.capacity + unit - 1) // unit    # (of a table that is wider than the capacity, all)
             self.bounds, self.bound_scales = new(B, Hkv, nb, 2, D, dtype=torch.int8), new(B, Hkv, nb, dtype=torch.float32)
 
     bound = property(lambda self: self.cache.S, lambda self, n: setattr(self.cache, "S", n),

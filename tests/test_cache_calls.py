@@ -273,3 +273,18 @@ def test_a_drop_takes_any_whole_number():
     with pytest.raises(ValueError, match="negative"):
         c.drop(np.int32(-1))
     assert c.lengths.tolist() == [37, 37] and c.bound == 37
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("unit", [0, 8])
+def test_a_block_table_wider_than_the_capacity(unit):
+    table = torch.tensor([[3, 0, 5], [1, 4, 2]], dtype=torch.int32, device="cuda")
+    c, plain = KVCache(2, 2, 32, 64, block_size=16, block_table=table, n_blocks=6, unit=unit), KVCache(2, 2, 32, 64, unit=unit)
+    k, q = values((2, 2, 30, 64), 1).cuda(), values((2, 4, 1, 64), 2).cuda()
+    for x in (c, plain):
+        x.append(k, k)
+    for n_select in {0, unit and 3}:
+        for x, y in zip(*(m.attend(q, n_select=n_select) for m in (c, plain))):
+            assert torch.equal(x, y)
+    with pytest.raises(ValueError, match="capacity"):
+        c.append(k, k)
