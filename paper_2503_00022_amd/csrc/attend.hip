@@ -29,13 +29,13 @@ namespace {
 
 using namespace kvc::cache;
 using kvc::tiles::kLn2;
-using kvc::tiles::kNegBig;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAhead = 512;         // keys whose places a wave looks up at once
+constexpr float kNegBig = -3.0e38f;  // reference of a row that has seen nothing yet: finite, and below what logits come to
 
 struct AttendParams {
   View c;

@@ -213,3 +213,23 @@ def test_infinities_in_chosen_and_other_blocks(fmt, Hq, Hkv, T):
             at = 5 if fmt in ref.DTYPES else slice(None)
             out[b, :Hq // Hkv, t, at] = want[b, :Hq // Hkv, t, at]
     check_attention(c, q, (torch.from_numpy(out), got[1]), n_new, lists=lists, unit=unit)
+
+
+@pytest.mark.parametrize("fmt", ref.FORMATS)
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("L", [50, 2500])
+def test_logits_far_below_zero(fmt, rows, L):
+    """All of a row's logits are about -10^33 but for one of half that: it is all of the softmax, not a row that sees nothing."""
+    Hq, Hkv, T = rows
+    D, rng = 64, np.random.RandomState(L)
+    big = 6e4 if fmt == "f16" else 2.0 ** 56
+    k, v = np.full((1, Hkv, L, D), -big, dtype=np.float32), rng.randn(1, Hkv, L, D).astype(np.float32)
+    k[:, :, L // 3] = -big / 2
+    c = made(fmt, k, v)
+    q = torch.full((1, Hq, T, D), 2.0 ** 15 if fmt == "f16" else 2.0 ** 53).to(ref.DTYPES[q_type(fmt)])
+    out, lse = kv.kvcrush_attend(c.make(kv), q.cuda())
+    want = ref.attend(q.double().numpy(), c.rows64["k"], c.rows64["v"], [L], [T])
+    # (other keys' weights are 0 in any arithmetic; lse: the logit's own rounding, D products and their sum)
+    half = torch.finfo(q.dtype).eps / 2
+    assert (np.abs(out.cpu().double().numpy() - want[0]) <= (half + 2.0 ** -16) * np.abs(want[0]) + 2.0 ** -17 * np.abs(c.rows64["v"]).max()).all()
+    assert (np.abs(lse.cpu().double().numpy() / want[1] - 1) <= 2.0 ** -18).all()
