@@ -159,18 +159,18 @@ __device__ __forceinline__ void k_frags(const char* tile, int lane, int u, u32x4
       const u32x4 w = *(const u32x4*)(tile + F::chunk_at(row, 4 * j + g));
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const u32x2 a = codes4_to_f16<F::FORMAT>(w[2 * i]), b = codes4_to_f16<F::FORMAT>(w[2 * i + 1]);
+        const u32x2 a = codes4_to_f16<F::FORMAT, true>(w[2 * i]), b = codes4_to_f16<F::FORMAT, true>(w[2 * i + 1]);
         f[2 * j + i] = u32x4{a[0], a[1], b[0], b[1]};
       }
     }
   } else if constexpr (F::kChunks == 4) {
     const u32x4 w = *(const u32x4*)(tile + F::chunk_at(row, g));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = codes8_to_f16(w[i]);
+    for (int i = 0; i < 4; ++i) f[i] = codes8_to_small_f16(w[i]);
   } else {
     const u32x2 w = *(const u32x2*)(tile + F::chunk_at(row, g >> 1) + (g & 1) * 8);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) f[i] = codes8_to_f16(w[i]);
+    for (int i = 0; i < 2; ++i) f[i] = codes8_to_small_f16(w[i]);
   }
 }
 // First value of the eight (four of a 32-bit type) that this lane's step t of the inner axis has.
@@ -315,7 +315,7 @@ __device__ __forceinline__ Sums<D> key_by_key(int b, int h, int t_list, int n, c
   const Slots slots = key_slots(p, b, h, t_list, n);
   last = min(last, slots.n);
   const size_t base = p.c.base(b, h), step = p.c.step();
-  const float scale = fmaxf(p.scale_log2, 0x1p-100f), room = (float)(33 - __builtin_clz(max(last - first, 1)));
+  const float scale = fmaxf(p.scale_log2, 0x1p-149f), room = (float)(33 - __builtin_clz(max(last - first, 1)));
   Sums<D> y;
   float q[kTogether][8];
   int t_of[kTogether];
@@ -579,14 +579,15 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
     const int t = p.blocks ? t_list : rr / p.G, head = h * p.G + (p.blocks ? rr : rr - t * p.G);
     t_of[c] = t;
     const char* q = p.q + ((size_t)b * p.q_stride[0] + (size_t)head * p.q_stride[1] + (size_t)t * p.q_stride[2]) * (format_bits(p.q_dtype) / 8);
-    col_scale[c] = fmaxf(p.scale_log2, 0x1p-100f);  // (never zero: what a row does not see is -infinity times this)
+    col_scale[c] = fmaxf(p.scale_log2, 0x1p-149f);  // (never zero: what a row does not see is -infinity times this)
     q_sum[c] = 0.0f;
     if constexpr (!F::kQuant) {
 #pragma unroll
       for (int j = 0; j < kQRegs; ++j) qf[c][j] = *(const u32x4*)(q + step_value<F>(g, j) * (F::kBits / 8));
     } else {
       // Halves for every type of query: a row is scaled by the power of two that brings its largest value to
-      // 2^14 .. 2^15, so that a bfloat16 value loses nothing unless it is 2^-29 of the largest.
+      // 2^14 .. 2^15, so that a bfloat16 value loses nothing unless it is 2^-29 of the largest.  K's codes come times 2^-14
+      // (kCodeFactor), so that products with large keys stay below fp32's largest.
       float x[F::kSteps][8];
       uint32_t top = 0;
 #pragma unroll
@@ -607,8 +608,8 @@ __global__ __launch_bounds__(F::waves(NC, RW) * KVC_WAVE) void attend_kernel(Att
       q_sum[c] = row_sum(q_sum[c]);
       const int up = min(141 - (int)(top >> 23), 126);  // >= -114
       const float by = __builtin_amdgcn_ldexpf(1.0f, up);
-      q_sum[c] *= by;
-      col_scale[c] = fmaxf(p.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, -up), 0x1p-120f);
+      q_sum[c] *= by * kCodeFactor;
+      col_scale[c] = fminf(fmaxf(__builtin_amdgcn_ldexpf(p.scale_log2, 14 - up), 0x1p-149f), 0x1p127f);
       constexpr int kOrder[2][8] = {{0, 1, 2, 3, 4, 5, 6, 7}, {0, 4, 1, 5, 2, 6, 3, 7}};
       constexpr int o = FORMAT == KVCRUSH_I4 ? 1 : 0;
 #pragma unroll

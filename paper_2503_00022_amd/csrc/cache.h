@@ -160,17 +160,19 @@ __device__ __forceinline__ void store8(char* at, const float (&x)[8]) {
   }
 }
 
-// Four 8-bit codes as halves, exactly.  Integers: code + 128 behind the exponent of 1024, less 1152.
-template <int FORMAT>
+// Four 8-bit codes as halves, exactly; SMALL: times kCodeFactor.  Integers: code + 128 behind the exponent of 1024, less 1152.
+constexpr float kCodeFactor = 0x1p-14f;
+template <int FORMAT, bool SMALL = false>
 __device__ __forceinline__ u32x2 codes4_to_f16(uint32_t w) {
+  constexpr float kBy = SMALL ? kCodeFactor : 1.0f;
   if constexpr (FORMAT == KVCRUSH_E4M3) {
-    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true))};
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, kBy, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, kBy, true))};
   } else {
     w ^= 0x80808080u;
-    const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-    const f16x2 lo = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + off;
-    const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) + off;
+    const f16x2 by = {(_Float16)kBy, (_Float16)kBy}, off = {(_Float16)(-1152.0f * kBy), (_Float16)(-1152.0f * kBy)};
+    const f16x2 lo = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)), by, off);
+    const f16x2 hi = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)), by, off);
     return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
   }
 }
@@ -198,13 +200,13 @@ __device__ __forceinline__ u32x4 codes8_to_bf16(uint32_t w) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, false)),
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, 512.0f, true))};
 }
-// Eight 4-bit codes as halves, exactly, in the order 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ u32x4 codes8_to_f16(uint32_t w) {
-  const f16x2 off = {(_Float16)-1024.0f, (_Float16)-1024.0f};
+// Eight 4-bit codes times kCodeFactor as halves, exactly, in the order 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ u32x4 codes8_to_small_f16(uint32_t w) {
+  const f16x2 by = {(_Float16)kCodeFactor, (_Float16)kCodeFactor}, off = {(_Float16)(-1024.0f * kCodeFactor), (_Float16)(-1024.0f * kCodeFactor)};
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000F000Fu) | 0x64006400u) + off);
+    r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000F000Fu) | 0x64006400u), by, off));
   return r;
 }
 

@@ -233,3 +233,39 @@ def test_logits_far_below_zero(fmt, rows, L):
     half = torch.finfo(q.dtype).eps / 2
     assert (np.abs(out.cpu().double().numpy() - want[0]) <= (half + 2.0 ** -16) * np.abs(want[0]) + 2.0 ** -17 * np.abs(c.rows64["v"]).max()).all()
     assert (np.abs(lse.cpu().double().numpy() / want[1] - 1) <= 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f32", "e4m3", "i8", "i4"])
+@pytest.mark.parametrize("rows", ROWS[1:3])
+@pytest.mark.parametrize("orders,scale", [(118, None), (-118, None), (60, 2.0 ** -110), (57, 2.0 ** -114)])
+def test_queries_and_keys_of_opposite_sizes(fmt, rows, orders, scale):
+    """Tiny queries and huge keys, the other way round, and huge ones of both with a tiny scale: ordinary logits."""
+    Hq, Hkv, T = rows
+    D, L, rng = 64, 300, np.random.RandomState(3)
+    k = (rng.randn(1, Hkv, L, D) * 2.0 ** orders).astype(np.float32)
+    v = rng.randn(1, Hkv, L, D).astype(np.float32)
+    if scale is None and orders < 0 and fmt in ("e4m3", "i8", "i4"):
+        k *= 2.0 ** 25                                         # (rows below 2^-100 are stored as zero)
+    c = made(fmt, k, v)
+    small = -orders if scale is None else -orders - math.log2(scale) - 3
+    q = (torch.from_numpy(rng.randn(1, Hq, T, D)) * 2.0 ** small).to(ref.DTYPES[q_type(fmt)])
+    check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda(), scale=scale or 0.0), [T], scale=scale)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "i8", "i4"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_small_codes_beside_a_large_one(fmt, rows):
+    """Each row of K has one value that makes its scale and that no query looks at; the logits are those of its smallest codes."""
+    Hq, Hkv, T = rows
+    D, L, rng = 128, 300, np.random.RandomState(4)
+    top = {"e4m3": 448.0, "i8": 127.0, "i4": 15.0}[fmt]
+    step = 2.0 ** -9 if fmt == "e4m3" else 1.0
+    k = (rng.randint(0, 8, (1, Hkv, L, D)) * step).astype(np.float32)
+    k[..., 0], k[..., 1] = top, 0.0
+    v = (rng.randint(0, 8, (1, Hkv, L, D)) * step).astype(np.float32)
+    v[..., 0], v[..., 1] = top, 0.0
+    c = made(fmt, k, v)
+    assert np.array_equal(c.rows64["k"], k) and np.array_equal(c.rows64["v"], v)
+    q = values((1, Hq, T, D), "bf16", 8, 0.3 / step)
+    q[..., 0] = 0
+    check_attention(c, q, kv.kvcrush_attend(c.make(kv), q.cuda()), [T])
